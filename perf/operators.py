@@ -3,7 +3,7 @@
 Five kinds of case, each one call:
 
   quantize  ``Context.quantize_fp8``: codes in e4m3 with an fp32 scale for each block, 1 x 128 (activations) or
-            128 x 128 (weights).  scale = max(largest magnitude / 448, 2^-126), code = round(x / scale).
+            128 x 128 (weights).  scale = max(largest magnitude / 448, 2^-126), code = round(x * (1 / scale)).
   gemm      ``Context.gemm_fp8``: y = act(sum over blocks of sa * sb * (a . b) + bias), rows of ``a`` against filters
             ``b`` stored [out][in]
   route     ``Context.route_experts``: scores of all experts, top-k of each row, and the rows sorted by expert
@@ -223,7 +223,7 @@ def _plain_quantize(case, s):
     R, C = s["x"].shape
     x = _blocks(s["x"].float(), case["block_rows"])
     scale = (x.abs().amax(dim=(1, 3)) / _TOP).clamp(min=_TINY)
-    codes = (x / scale[:, None, :, None]).clamp(-_TOP, _TOP).reshape(-1, x.shape[2] * 128)[:R, :C]
+    codes = (x * (1.0 / scale)[:, None, :, None]).clamp(-_TOP, _TOP).reshape(-1, x.shape[2] * 128)[:R, :C]
     return codes.to(torch.float8_e4m3fn), scale
 
 
