@@ -69,6 +69,8 @@ enum {
 
 enum { PSB_LAYOUT_NCHW = 0, PSB_LAYOUT_NHWC = 1 };
 enum { PSB_DT_U8 = 0, PSB_DT_S8 = 1 };
+/* Real-valued types of the layers in 8-bit floating point (below). */
+enum { PSB_DT_F32 = 2, PSB_DT_BF16 = 3, PSB_DT_F16 = 4, PSB_DT_E4M3 = 5, PSB_DT_E5M2 = 6 };
 
 /* Which contraction kernel a conv / gemm call uses. */
 enum {
@@ -403,6 +405,113 @@ psb_status psb_run(psb_ctx* ctx, const psb_op* ops, uint32_t n_ops, void* stream
 psb_status psb_sample_level_static(const float* w_dev, const psb_wshape* shape,
                                    const psb_sample_cfg* cfg, uint32_t log2k, int32_t* wint_out_dev,
                                    int32_t* e_base_out_dev, void* stream);
+
+/* Layers in 8-bit floating point, and experts (no counterpart in the paper).
+ *
+ * A network that runs next to sampled layers keeps some of its layers real-valued and not sampled, in 8-bit
+ * floating point with an fp32 scale for each block of 128 values along the reduction axis; and where a draw-count
+ * map decides per location how exactly a filter is sampled, a router decides per row which of several filters
+ * ("experts") it meets at all.
+ *
+ * Conventions of these five calls: matrices are row-major, elements of a row follow one another, rows are `*_stride`
+ * elements apart (0: as many as a row has; blocks of a scale row likewise).  Strides may exceed the row; what
+ * lies between rows is neither read nor written.  Nothing is allocated except by psb_route_experts (scratch, see the
+ * top of this file).  They run on the context's device, which becomes the current one. */
+
+/* Codes and scales of a matrix.  Per block of block_rows x 128 (1: activations, 128: filters; blocks at the ends are
+ * cut off):
+ *   top   = 448 (PSB_DT_E4M3) or 57344 (PSB_DT_E5M2)
+ *   scale = max(max |x| / top, 2^-126)      over the block's finite values, fp32
+ *   code  = round(x * (1 / scale))          ties to even, saturating at +-top; Inf and NaN become NaN
+ * codes_dev: one byte each; scales_dev: [ceil(rows / block_rows)][ceil(cols / 128)].
+ * Rows of codes that psb_gemm_fp8 is to read start at multiples of 16 bytes. */
+typedef struct {
+  uint32_t in_dtype;        /* PSB_DT_F32, PSB_DT_BF16, PSB_DT_F16 */
+  uint32_t code_dtype;      /* PSB_DT_E4M3, PSB_DT_E5M2 */
+  uint32_t rows, cols;
+  uint32_t block_rows;      /* 1 or 128 */
+  uint32_t reserved;        /* 0 */
+  uint64_t x_stride, code_stride, scale_stride;
+} psb_quantize_desc;
+psb_status psb_quantize_fp8(psb_ctx* ctx, const void* x_dev, const psb_quantize_desc* desc, uint8_t* codes_dev,
+                            float* scales_dev, void* stream);
+
+/* Fully connected layer of codes:
+ *   y[m][n] = sum_b a_scale[m][b] * b_scale[n / 128][b] * sum_{k in block b} a[m][k] * b[n][k]   (+ bias[n])
+ *   y = 0 if relu and y < 0;  rounded once to out_dtype
+ * The sum of a block is accumulated in fp32 by the tensor cores, the scaled sums in fp32 in the order of the blocks (where
+ * few rows leave SMs idle the blocks are cut into parts, whose sums are added in order: the same call gives the same bits).
+ *   a_dev [m][k], b_dev [n][k]   codes; addresses and strides are multiples of 16 (PSB_ERR_INVALID_ARG otherwise)
+ *   a_scale_dev [m][ceil(k / 128)], b_scale_dev [ceil(n / 128)][ceil(k / 128)], bias_dev fp32 [n] or NULL, out_dev [m][n]
+ * NaN codes give NaN (with relu too), infinities of PSB_DT_E5M2 follow the arithmetic of the sum. */
+typedef struct {
+  uint32_t a_dtype, b_dtype;  /* PSB_DT_E4M3, PSB_DT_E5M2, each */
+  uint32_t out_dtype;         /* PSB_DT_F32, PSB_DT_BF16, PSB_DT_F16 */
+  uint32_t m, n, k;
+  uint32_t relu;
+  uint32_t reserved;          /* 0 */
+  uint64_t a_stride, b_stride, a_scale_stride, b_scale_stride, out_stride;
+  const float* bias_dev;
+} psb_gemm_fp8_desc;
+psb_status psb_gemm_fp8(psb_ctx* ctx, const uint8_t* a_dev, const float* a_scale_dev, const uint8_t* b_dev,
+                        const float* b_scale_dev, void* out_dev, const psb_gemm_fp8_desc* desc, void* stream);
+
+/* The same against the filter of each row's expert.  Output rows offsets[e] .. offsets[e + 1] - 1 belong to expert e; row r
+ * reads row order[r] of a (order_dev NULL: row r).  desc->m is the number of rows of a; out has `rows` rows, and those
+ * behind offsets[experts] are left as they were.
+ *   offsets_dev int32 [experts + 1], not decreasing, from 0 to at most `rows`; order_dev int32 [rows] or NULL (rows <= desc->m)
+ *   b [experts][n][k], b_scale [experts][ceil(n / 128)][ceil(k / 128)], bias [experts][n] or NULL; experts are
+ *   b_expert_stride, b_scale_expert_stride elements apart (0: rows x stride), biases n.
+ * experts <= 1024.  Offsets that decrease or leave [0, rows] and rows that a does not have raise PSB_ERR_RANGE through
+ * psb_device_status; their outputs are unspecified, and nothing outside the tensors is touched. */
+typedef struct {
+  psb_gemm_fp8_desc gemm;
+  uint32_t experts, rows;
+  uint64_t b_expert_stride, b_scale_expert_stride;
+} psb_gemm_fp8_experts_desc;
+psb_status psb_gemm_fp8_experts(psb_ctx* ctx, const uint8_t* a_dev, const float* a_scale_dev, const uint8_t* b_dev,
+                                const float* b_scale_dev, const int32_t* offsets_dev, const int32_t* order_dev,
+                                void* out_dev, const psb_gemm_fp8_experts_desc* desc, void* stream);
+
+/* Which experts each row goes to, with what weights, and the rows in the order of the experts.
+ *   available: experts whose logit is neither -inf nor NaN (+inf counts as the largest fp32 number)
+ *   score     softmax over the available experts, or sigmoid
+ *   select    score + bias (bias_dev NULL: score), compared as in 64 bits, equal values by the lower index; without a bias and
+ *             groups by the logits.  An expert whose bias is NaN is not chosen.
+ *   groups    experts / groups consecutive experts each; a group's strength is the sum of its group_best (1 or 2) largest
+ *             select values among available experts; only experts of the top_groups strongest groups stay
+ *   ids       the top_k largest select values in falling order; -1 where fewer experts are available
+ *   weights   scaling * score, with renormalise divided by the sum of the row's chosen scores; 0 where ids is -1
+ * token_mask_dev u8 [tokens] or NULL: rows with 0 choose nothing (ids -1, weights 0), whatever their logits hold.
+ *   ids_dev int32 [tokens][top_k], weights_dev fp32 [tokens][top_k]
+ *   offsets_dev int32 [experts + 1], order_dev int32 [tokens * top_k], slot_dev int32 [tokens][top_k]: the choices sorted
+ *   by expert, within an expert by row; order[r] is the row behind place r (-1 behind the last), slot the place of each choice
+ *   (-1 where ids is).  All three or none (NULL).
+ * experts <= 1024, top_k <= 32, tokens * top_k < 2^31. */
+enum { PSB_SCORE_SOFTMAX = 0, PSB_SCORE_SIGMOID = 1 };
+typedef struct {
+  uint32_t in_dtype;          /* PSB_DT_F32, PSB_DT_BF16, PSB_DT_F16 */
+  uint32_t score;
+  uint32_t tokens, experts, top_k;
+  uint32_t groups, top_groups, group_best;   /* 1, 1, 1: no groups */
+  uint32_t renormalise;
+  float scaling;
+  uint64_t logit_stride;
+} psb_route_desc;
+psb_status psb_route_experts(psb_ctx* ctx, const void* logits_dev, const float* bias_dev, const uint8_t* token_mask_dev,
+                             const psb_route_desc* desc, int32_t* ids_dev, float* weights_dev, int32_t* offsets_dev,
+                             int32_t* order_dev, int32_t* slot_dev, void* stream);
+
+/* The chosen experts' rows put together:  out[t] = sum_j weights[t][j] * y[slot[t][j]]  over the choices with
+ * slot >= 0, in fp32 in the order of j, rounded once (0 where there is none).  y has `rows` rows of n; a slot beyond
+ * them raises PSB_ERR_RANGE through psb_device_status and contributes nothing.  top_k <= 32. */
+typedef struct {
+  uint32_t in_dtype, out_dtype;   /* PSB_DT_F32, PSB_DT_BF16, PSB_DT_F16, each */
+  uint32_t tokens, top_k, n, rows;
+  uint64_t y_stride, out_stride;
+} psb_combine_desc;
+psb_status psb_combine_experts(psb_ctx* ctx, const void* y_dev, const float* weights_dev, const int32_t* slot_dev,
+                               const psb_combine_desc* desc, void* out_dev, void* stream);
 
 #ifdef __cplusplus
 }

@@ -20,6 +20,8 @@ PSB_ERR_CUDA, PSB_ERR_TIMEOUT, PSB_ERR_NONFINITE_WEIGHT, PSB_ERR_RANGE = -5, -6,
 PSB_CHECK_RANGE = 1
 PSB_LAYOUT_NCHW, PSB_LAYOUT_NHWC = 0, 1
 PSB_DT_U8, PSB_DT_S8 = 0, 1
+PSB_DT_F32, PSB_DT_BF16, PSB_DT_F16, PSB_DT_E4M3, PSB_DT_E5M2 = 2, 3, 4, 5, 6
+PSB_SCORE_SOFTMAX, PSB_SCORE_SIGMOID = 0, 1
 PSB_PATH_AUTO, PSB_PATH_SHIFT_ADD, PSB_PATH_TENSOR = 0, 1, 2
 
 EXPORTS = ["psb_create", "psb_destroy", "psb_status_string", "psb_device_status", "psb_sample_weights",
@@ -28,7 +30,8 @@ EXPORTS = ["psb_create", "psb_destroy", "psb_status_string", "psb_device_status"
            "psb_sample_batch_create", "psb_sample_batch_run", "psb_sample_batch_free", "psb_run",
            "psb_launch_count", "psb_int8_mma_probe", "psb_contraction_timing", "psb_contraction_time",
            "psb_set_checks", "psb_set_wait_limit", "psb_wait_selftest", "psb_contraction_times",
-           "psb_attention_entropy", "psb_attention_maps"]
+           "psb_attention_entropy", "psb_attention_maps", "psb_quantize_fp8", "psb_gemm_fp8", "psb_gemm_fp8_experts",
+           "psb_route_experts", "psb_combine_experts"]
 
 
 class psb_wshape(C.Structure):
@@ -68,6 +71,32 @@ class psb_op(C.Structure):
                 ("pool_qmax", C.c_int32), ("pool_out_dev", C.c_void_p)]
 
 
+class psb_quantize_desc(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("in_dtype", "code_dtype", "rows", "cols", "block_rows", "reserved")] + [
+        (n, C.c_uint64) for n in ("x_stride", "code_stride", "scale_stride")]
+
+
+class psb_gemm_fp8_desc(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("a_dtype", "b_dtype", "out_dtype", "m", "n", "k", "relu", "reserved")] + [
+        (n, C.c_uint64) for n in ("a_stride", "b_stride", "a_scale_stride", "b_scale_stride", "out_stride")] + [
+        ("bias_dev", C.c_void_p)]
+
+
+class psb_gemm_fp8_experts_desc(C.Structure):
+    _fields_ = [("gemm", psb_gemm_fp8_desc), ("experts", C.c_uint32), ("rows", C.c_uint32),
+                ("b_expert_stride", C.c_uint64), ("b_scale_expert_stride", C.c_uint64)]
+
+
+class psb_route_desc(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("in_dtype", "score", "tokens", "experts", "top_k", "groups", "top_groups", "group_best",
+                                          "renormalise")] + [("scaling", C.c_float), ("logit_stride", C.c_uint64)]
+
+
+class psb_combine_desc(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("in_dtype", "out_dtype", "tokens", "top_k", "n", "rows")] + [
+        ("y_stride", C.c_uint64), ("out_stride", C.c_uint64)]
+
+
 PSB_OP_CONV2D, PSB_OP_GEMM, PSB_OP_MAXPOOL, PSB_OP_AVGPOOL = 0, 1, 2, 3
 
 # The argument blocks of the calls that a program makes once per layer, packed in one go: filling the ctypes structures
@@ -76,6 +105,11 @@ PSB_OP_CONV2D, PSB_OP_GEMM, PSB_OP_MAXPOOL, PSB_OP_AVGPOOL = 0, 1, 2, 3
 _EP_FMT = "3QfIIfiiI4x3Q"
 _CONV_BLOCK, _GEMM_BLOCK = struct.Struct("=10I" + _EP_FMT), struct.Struct("=5I4x" + _EP_FMT)
 _SHAPE_BLOCK, _CFG_BLOCK = struct.Struct("=5I"), struct.Struct("=Q8I")
+_QUANT_BLOCK, _ROUTE_BLOCK, _COMBINE_BLOCK = struct.Struct("=6I3Q"), struct.Struct("=9If1Q"), struct.Struct("=6I2Q")
+_GEMM_FP8_BLOCK, _EXPERTS_BLOCK = struct.Struct("=8I6Q"), struct.Struct("=8I6Q2I2Q")
+assert _QUANT_BLOCK.size == C.sizeof(psb_quantize_desc) and _ROUTE_BLOCK.size == C.sizeof(psb_route_desc)
+assert _GEMM_FP8_BLOCK.size == C.sizeof(psb_gemm_fp8_desc) and _EXPERTS_BLOCK.size == C.sizeof(psb_gemm_fp8_experts_desc)
+assert _COMBINE_BLOCK.size == C.sizeof(psb_combine_desc)
 assert _CONV_BLOCK.size == C.sizeof(psb_conv_desc) and _GEMM_BLOCK.size == C.sizeof(psb_gemm_desc)
 assert _SHAPE_BLOCK.size == C.sizeof(psb_wshape) and _CFG_BLOCK.size == C.sizeof(psb_sample_cfg)
 
@@ -134,6 +168,15 @@ def load_library():
     lib.psb_sample_batch_run.argtypes = [vp, vp, C.c_uint64, vp]
     lib.psb_sample_batch_free.argtypes = [vp, vp]
     lib.psb_run.argtypes = [vp, C.POINTER(psb_op), u32, vp]
+    lib.psb_quantize_fp8.argtypes = [vp, vp, C.POINTER(psb_quantize_desc), vp, vp, vp]
+    lib.psb_gemm_fp8.argtypes = [vp, vp, vp, vp, vp, vp, C.POINTER(psb_gemm_fp8_desc), vp]
+    lib.psb_gemm_fp8_experts.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, C.POINTER(psb_gemm_fp8_experts_desc), vp]
+    lib.psb_route_experts.argtypes = [vp, vp, vp, vp, C.POINTER(psb_route_desc), vp, vp, vp, vp, vp, vp]
+    lib.psb_combine_experts.argtypes = [vp, vp, vp, vp, C.POINTER(psb_combine_desc), vp, vp]
+    for name in ("quantize_fp8", "gemm_fp8", "gemm_fp8_experts", "route_experts", "combine_experts"):
+        packed = lib["psb_" + name]
+        packed.argtypes, packed.restype = [vp] * len(getattr(lib, "psb_" + name).argtypes), i32
+        setattr(lib, "packed_" + name, packed)
     for name in EXPORTS:
         if name not in ("psb_status_string", "psb_launch_count"):
             getattr(lib, name).restype = i32
@@ -174,6 +217,27 @@ def _dt_of(t):
     if t.dtype == torch.int8:
         return PSB_DT_S8
     raise TypeError("activations must be uint8 or int8")
+
+
+_REAL_DT = {torch.float32: PSB_DT_F32, torch.bfloat16: PSB_DT_BF16, torch.float16: PSB_DT_F16}
+_CODE_DT = {torch.float8_e4m3fn: PSB_DT_E4M3, torch.float8_e5m2: PSB_DT_E5M2}
+_SCORES = {"softmax": PSB_SCORE_SOFTMAX, "sigmoid": PSB_SCORE_SIGMOID}
+
+
+def _on(t, device, what):
+    if t.device != device:
+        raise ValueError("%s is on %s, the context on %s" % (what, t.device, device))
+
+
+def _rows(t, multiple=1):
+    """Elements between the rows of a matrix whose row elements follow one another."""
+    rows, cols = t.shape[-2:]
+    stride, step = t.stride()[-2:]
+    if cols > 1 and step != 1:
+        raise ValueError("the elements of a row must follow one another")
+    if rows > 1:
+        return stride
+    return -(-cols // multiple) * multiple
 
 
 PSB_STATIC_MAX_OUT_CH = 4096
@@ -386,6 +450,140 @@ class Context:
         _check(self.lib.psb_attention_maps(self.handle, _ptr(entropy), n, h, w, lo_log2k, hi_log2k, len(res), ra, pa,
                                            _ptr(mean), _stream(stream)), "psb_attention_maps")
         return maps, mean
+
+    # -- layers in 8-bit floating point, experts ---------------------------------
+    def quantize_fp8(self, x, block_rows=1, code_dtype=torch.float8_e4m3fn, out=None, stream=None):
+        """x: float32/bfloat16/float16 CUDA tensor [rows, cols].  Returns (codes, scales): codes [rows, cols] of code_dtype,
+        rows 16 bytes or a multiple apart, scales float32 [ceil(rows / block_rows), ceil(cols / 128)].  block_rows: 1 for
+        activations, 128 for filters; out: (codes, scales) to write to."""
+        _on(x, self.device, "x")
+        rows, cols = x.shape
+        blocks = (cols + 127) // 128
+        if out is None:
+            codes = torch.empty((rows, (cols + 15) & ~15), dtype=code_dtype, device=self.device)
+            if cols & 15:
+                codes = codes[:, :cols]
+            scales = torch.empty(((rows + block_rows - 1) // block_rows, blocks), dtype=torch.float32, device=self.device)
+        else:
+            codes, scales = out
+            _on(codes, self.device, "codes"), _on(scales, self.device, "scales")
+            assert codes.shape == x.shape and scales.dtype == torch.float32
+            assert tuple(scales.shape) == ((rows + block_rows - 1) // block_rows, blocks)
+        d = _block(_QUANT_BLOCK, psb_quantize_desc, (_REAL_DT[x.dtype], _CODE_DT[codes.dtype], rows, cols, block_rows, 0,
+                                                     _rows(x), _rows(codes), _rows(scales)))
+        _check(self.lib.packed_quantize_fp8(self.handle, x.data_ptr(), d, codes.data_ptr(), scales.data_ptr(), _stream(stream)),
+               "psb_quantize_fp8")
+        return codes, scales
+
+    def _gemm_fp8_head(self, a, a_scale, b, b_scale, bias, relu, out, rows):
+        m, k = a.shape
+        n = b.shape[-2]
+        blocks = (k + 127) // 128
+        for t, what in ((a, "a"), (a_scale, "a_scale"), (b, "b"), (b_scale, "b_scale"), (out, "out")):
+            _on(t, self.device, what)
+        assert a_scale.dtype == b_scale.dtype == torch.float32
+        if b.shape[-1] != k or tuple(a_scale.shape) != (m, blocks) or tuple(b_scale.shape[-2:]) != ((n + 127) // 128, blocks):
+            raise ValueError("codes and scales do not fit together")
+        if tuple(out.shape) != (rows, n):
+            raise ValueError("out must be [%d, %d]" % (rows, n))
+        if bias is not None:
+            _on(bias, self.device, "bias")
+            if bias.dtype != torch.float32 or not bias.is_contiguous() or bias.shape[-1] != n or bias.dim() != b.dim() - 1:
+                raise ValueError("bias must be float32, one for each output")
+        return (_CODE_DT[a.dtype], _CODE_DT[b.dtype], _REAL_DT[out.dtype], m, n, k, 1 if relu else 0, 0, _rows(a, 16), _rows(b, 16),
+                _rows(a_scale), _rows(b_scale), _rows(out), 0 if bias is None else bias.data_ptr())
+
+    def gemm_fp8(self, a, a_scale, b, b_scale, bias=None, relu=False, out_dtype=torch.bfloat16, out=None, stream=None):
+        """Rows of codes a [m, k] against a filter b [n, k] (see quantize_fp8): scales [m, ceil(k / 128)] and
+        [ceil(n / 128), ceil(k / 128)], bias float32 [n].  Returns [m, n] of out_dtype (or `out`)."""
+        if out is None:
+            out = torch.empty((a.shape[0], b.shape[0]), dtype=out_dtype, device=self.device)
+        assert a.dim() == b.dim() == 2
+        d = _GEMM_FP8_BLOCK.pack(*self._gemm_fp8_head(a, a_scale, b, b_scale, bias, relu, out, a.shape[0]))
+        _check(self.lib.packed_gemm_fp8(self.handle, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), out.data_ptr(), d,
+                                        _stream(stream)), "psb_gemm_fp8")
+        return out
+
+    def gemm_fp8_experts(self, a, a_scale, b, b_scale, offsets, order=None, bias=None, relu=False, out_dtype=torch.bfloat16, out=None,
+                         stream=None):
+        """Output rows offsets[e] .. offsets[e + 1] - 1 are rows of a against filter e of b [experts, n, k], with scales
+        [experts, ceil(n / 128), ceil(k / 128)] and bias float32 [experts, n].  order int32 [rows] names the row of a behind each
+        output row (None: the same row).  offsets int32 [experts + 1]; both as route_experts gives them.  Rows
+        behind offsets[experts] are left as they are in `out` (undefined where it is made here)."""
+        assert a.dim() == 2 and b.dim() == 3 and b_scale.dim() == 3
+        rows = a.shape[0] if order is None else order.shape[0]
+        if out is None:
+            out = torch.empty((rows, b.shape[1]), dtype=out_dtype, device=self.device)
+        experts = b.shape[0]
+        for t in (offsets, order):
+            if t is not None:
+                _on(t, self.device, "offsets and order")
+                assert t.dtype == torch.int32 and t.is_contiguous() and t.dim() == 1
+        if offsets.shape[0] != experts + 1 or b_scale.shape[0] != experts:
+            raise ValueError("one more offset than experts, and scales of each")
+        head = self._gemm_fp8_head(a, a_scale, b, b_scale, bias, relu, out, rows)
+        d = _EXPERTS_BLOCK.pack(*head, experts, rows, b.stride(0) if experts > 1 else 0, b_scale.stride(0) if experts > 1 else 0)
+        _check(self.lib.packed_gemm_fp8_experts(self.handle, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(),
+                                                offsets.data_ptr(), 0 if order is None else order.data_ptr(), out.data_ptr(), d,
+                                                _stream(stream)), "psb_gemm_fp8_experts")
+        return out
+
+    def route_experts(self, logits, top_k, score="softmax", bias=None, groups=1, top_groups=1, group_best=1, renormalise=True, scaling=1.0,
+                      token_mask=None, sort=True, stream=None):
+        """logits: float32/bfloat16/float16 CUDA tensor [tokens, experts]; score "softmax" or "sigmoid"; bias float32 [experts] is added
+        for the choice alone; of `groups` runs of experts the top_groups with the largest sums of their group_best best stay;
+        token_mask uint8 [tokens], 0 for rows that choose nothing.  Returns a dict: ids int32 [tokens, top_k] (-1: none),
+        weights float32 [tokens, top_k] and, with `sort`, offsets int32 [experts + 1], order int32 [tokens * top_k], slot int32
+        [tokens, top_k] (see psb_route_experts)."""
+        _on(logits, self.device, "logits")
+        tokens, experts = logits.shape
+        if bias is not None:
+            _on(bias, self.device, "bias")
+            if bias.dtype != torch.float32 or not bias.is_contiguous() or tuple(bias.shape) != (experts,):
+                raise ValueError("bias must be float32 [experts]")
+        if token_mask is not None:
+            _on(token_mask, self.device, "token_mask")
+            if token_mask.dtype != torch.uint8 or not token_mask.is_contiguous() or tuple(token_mask.shape) != (tokens,):
+                raise ValueError("token_mask must be uint8 [tokens]")
+        if score not in _SCORES:
+            raise ValueError("score must be 'softmax' or 'sigmoid'")
+        n = tokens * top_k
+        # one allocation for the whole answer
+        words = torch.empty((3 * n + experts + 1 if sort else n,), dtype=torch.int32, device=self.device)
+        out = dict(ids=words[:n].view(tokens, top_k), weights=torch.empty((tokens, top_k), dtype=torch.float32, device=self.device))
+        at, offsets, order, slot = words.data_ptr(), 0, 0, 0
+        if sort:
+            out["slot"] = words[n:2 * n].view(tokens, top_k)
+            out["order"] = words[2 * n:3 * n]
+            out["offsets"] = words[3 * n:]
+            slot, order, offsets = at + 4 * n, at + 8 * n, at + 12 * n
+        d = _block(_ROUTE_BLOCK, psb_route_desc, (_REAL_DT[logits.dtype], _SCORES[score], tokens, experts, top_k, groups, top_groups,
+                                                  group_best, 1 if renormalise else 0, float(scaling), _rows(logits)))
+        _check(self.lib.packed_route_experts(self.handle, logits.data_ptr(), 0 if bias is None else bias.data_ptr(),
+                                             0 if token_mask is None else token_mask.data_ptr(), d, at, out["weights"].data_ptr(), offsets,
+                                             order, slot, _stream(stream)), "psb_route_experts")
+        return out
+
+    def combine_experts(self, y, weights, slot, out_dtype=None, out=None, stream=None):
+        """out[t] = sum over j of weights[t, j] * y[slot[t, j]], choices with slot -1 left out.  y [rows, n], weights float32 and
+        slot int32 [tokens, top_k] as route_experts gives them; out_dtype: that of y unless given."""
+        rows, n = y.shape
+        tokens, top_k = slot.shape
+        for t, what in ((y, "y"), (weights, "weights"), (slot, "slot")):
+            _on(t, self.device, what)
+        if weights.dtype != torch.float32 or slot.dtype != torch.int32 or weights.shape != slot.shape:
+            raise ValueError("weights float32 and slot int32, alike in shape")
+        if not (weights.is_contiguous() and slot.is_contiguous()):
+            raise ValueError("weights and slot must be contiguous")
+        if out is None:
+            out = torch.empty((tokens, n), dtype=out_dtype or y.dtype, device=self.device)
+        _on(out, self.device, "out")
+        if tuple(out.shape) != (tokens, n):
+            raise ValueError("out must be [%d, %d]" % (tokens, n))
+        d = _block(_COMBINE_BLOCK, psb_combine_desc, (_REAL_DT[y.dtype], _REAL_DT[out.dtype], tokens, top_k, n, rows, _rows(y), _rows(out)))
+        _check(self.lib.packed_combine_experts(self.handle, y.data_ptr(), weights.data_ptr(), slot.data_ptr(), d, out.data_ptr(),
+                                               _stream(stream)), "psb_combine_experts")
+        return out
 
     # -- whole networks -------------------------------------------------------
     def sample_batch_create(self, filters, weights):

@@ -143,6 +143,52 @@ psb_status check_epilogue(const psb_epilogue& ep) {
   return PSB_OK;
 }
 
+bool is_real(uint32_t dtype) { return dtype >= PSB_DT_F32 && dtype <= PSB_DT_F16; }
+bool is_code(uint32_t dtype) { return dtype == PSB_DT_E4M3 || dtype == PSB_DT_E5M2; }
+uint32_t size_of(uint32_t dtype) { return dtype == PSB_DT_F32 ? 4u : is_real(dtype) ? 2u : 1u; }
+bool misaligned(const void* p, uint32_t bytes) { return ((uintptr_t)p & (bytes - 1u)) != 0u; }
+// A row stride as given, or that of rows that follow one another; false if rows would overlap or pass 2^40 elements.
+bool row_stride(uint64_t& stride, uint64_t row) {
+  if (stride == 0u) stride = row;
+  return stride >= row && stride < (1ull << 40);
+}
+
+// Shared checks of psb_gemm_fp8 and psb_gemm_fp8_experts (experts: 0 for one filter); fills `g` but for the experts' part.
+psb_status check_gemm_fp8(const uint8_t* a, const float* a_scale, const uint8_t* b, const float* b_scale, void* out,
+                          const psb_gemm_fp8_desc& d, Fp8GemmArgs& g) {
+  if (!a || !a_scale || !b || !b_scale || !out || !d.m || !d.n || !d.k || d.reserved || d.relu > 1u) return PSB_ERR_INVALID_ARG;
+  if (!is_code(d.a_dtype) || !is_code(d.b_dtype) || !is_real(d.out_dtype)) return PSB_ERR_INVALID_ARG;
+  const uint64_t k_blocks = ((uint64_t)d.k + 127u) / 128u;
+  g = Fp8GemmArgs();
+  g.a_stride = d.a_stride;
+  g.b_stride = d.b_stride;
+  g.a_scale_stride = d.a_scale_stride;
+  g.b_scale_stride = d.b_scale_stride;
+  g.out_stride = d.out_stride;
+  if (!row_stride(g.a_stride, d.k) || !row_stride(g.b_stride, d.k) || !row_stride(g.a_scale_stride, k_blocks) ||
+      !row_stride(g.b_scale_stride, k_blocks) || !row_stride(g.out_stride, d.n))
+    return PSB_ERR_INVALID_ARG;
+  if (misaligned(a, 16) || misaligned(b, 16) || ((g.a_stride | g.b_stride) & 15u) || misaligned(a_scale, 4) || misaligned(b_scale, 4) ||
+      misaligned(d.bias_dev, 4) || misaligned(out, size_of(d.out_dtype)))
+    return PSB_ERR_INVALID_ARG;
+  if (d.m >= (1u << 31) || d.n >= (1u << 30) || d.k >= (1u << 30)) return PSB_ERR_UNSUPPORTED;
+  g.a = a;
+  g.a_scale = a_scale;
+  g.b = b;
+  g.b_scale = b_scale;
+  g.bias = d.bias_dev;
+  g.out = out;
+  g.a_dtype = d.a_dtype;
+  g.b_dtype = d.b_dtype;
+  g.out_dtype = d.out_dtype;
+  g.m = d.m;
+  g.n = d.n;
+  g.k = d.k;
+  g.relu = d.relu;
+  g.rows = d.m;
+  return PSB_OK;
+}
+
 // Shared body of psb_conv2d and psb_gemm.
 psb_status run_layer(psb_ctx* ctx, const psb_weights* wt, const void* x_dev, uint32_t layout,
                      uint32_t in_dtype, uint32_t in_max, uint32_t n, uint32_t c, uint32_t h,
@@ -744,6 +790,97 @@ psb_status psb_global_avgpool_u8(psb_ctx* ctx, const uint8_t* x_dev, uint32_t la
                      (cudaStream_t)stream) != cudaSuccess)
     return PSB_ERR_CUDA;
   return PSB_OK;
+}
+
+psb_status psb_quantize_fp8(psb_ctx* ctx, const void* x_dev, const psb_quantize_desc* desc, uint8_t* codes_dev,
+                            float* scales_dev, void* stream) {
+  if (!ctx || !x_dev || !desc || !codes_dev || !scales_dev) return PSB_ERR_INVALID_ARG;
+  psb_quantize_desc d = *desc;
+  if (!is_real(d.in_dtype) || !is_code(d.code_dtype) || !d.rows || !d.cols || d.reserved || (d.block_rows != 1u && d.block_rows != 128u))
+    return PSB_ERR_INVALID_ARG;
+  const uint64_t blocks = ((uint64_t)d.cols + 127u) / 128u;
+  if (!row_stride(d.x_stride, d.cols) || !row_stride(d.code_stride, d.cols) || !row_stride(d.scale_stride, blocks)) return PSB_ERR_INVALID_ARG;
+  if (misaligned(x_dev, size_of(d.in_dtype)) || misaligned(scales_dev, 4)) return PSB_ERR_INVALID_ARG;
+  if (d.cols >= (1u << 31) || d.rows >= (1u << 31) || ((uint64_t)d.rows + 127u) / 128u * blocks >= (1ull << 31)) return PSB_ERR_UNSUPPORTED;
+  cudaSetDevice(ctx->device);
+  return launch_quantize_fp8(x_dev, d, codes_dev, scales_dev, (cudaStream_t)stream) == cudaSuccess ? PSB_OK : PSB_ERR_CUDA;
+}
+
+psb_status psb_gemm_fp8(psb_ctx* ctx, const uint8_t* a_dev, const float* a_scale_dev, const uint8_t* b_dev,
+                        const float* b_scale_dev, void* out_dev, const psb_gemm_fp8_desc* desc, void* stream) {
+  if (!ctx || !desc) return PSB_ERR_INVALID_ARG;
+  Fp8GemmArgs g;
+  const psb_status st = check_gemm_fp8(a_dev, a_scale_dev, b_dev, b_scale_dev, out_dev, *desc, g);
+  if (st != PSB_OK) return st;
+  cudaSetDevice(ctx->device);
+  return launch_gemm_fp8(ctx, g, (cudaStream_t)stream);
+}
+
+psb_status psb_gemm_fp8_experts(psb_ctx* ctx, const uint8_t* a_dev, const float* a_scale_dev, const uint8_t* b_dev,
+                                const float* b_scale_dev, const int32_t* offsets_dev, const int32_t* order_dev,
+                                void* out_dev, const psb_gemm_fp8_experts_desc* desc, void* stream) {
+  if (!ctx || !desc || !offsets_dev || !desc->experts || !desc->rows) return PSB_ERR_INVALID_ARG;
+  Fp8GemmArgs g;
+  const psb_status st = check_gemm_fp8(a_dev, a_scale_dev, b_dev, b_scale_dev, out_dev, desc->gemm, g);
+  if (st != PSB_OK) return st;
+  if (misaligned(offsets_dev, 4) || misaligned(order_dev, 4)) return PSB_ERR_INVALID_ARG;
+  if (!order_dev && desc->rows > desc->gemm.m) return PSB_ERR_INVALID_ARG;
+  if (desc->experts > 1024u || desc->rows >= (1u << 31)) return PSB_ERR_UNSUPPORTED;
+  g.b_expert_stride = desc->b_expert_stride;
+  g.b_scale_expert_stride = desc->b_scale_expert_stride;
+  if (!row_stride(g.b_expert_stride, (uint64_t)g.n * g.b_stride - (g.b_stride - g.k)) && desc->experts > 1u) return PSB_ERR_INVALID_ARG;
+  if (!desc->b_expert_stride) g.b_expert_stride = (uint64_t)g.n * g.b_stride;
+  if (!row_stride(g.b_scale_expert_stride, ((uint64_t)g.n + 127u) / 128u * g.b_scale_stride)) return PSB_ERR_INVALID_ARG;
+  if ((g.b_expert_stride & 15u) || g.b_expert_stride >= (1ull << 40)) return PSB_ERR_INVALID_ARG;
+  g.experts = desc->experts;
+  g.rows = desc->rows;
+  g.offsets = offsets_dev;
+  g.order = order_dev;
+  cudaSetDevice(ctx->device);
+  return launch_gemm_fp8(ctx, g, (cudaStream_t)stream);
+}
+
+psb_status psb_route_experts(psb_ctx* ctx, const void* logits_dev, const float* bias_dev, const uint8_t* token_mask_dev,
+                             const psb_route_desc* desc, int32_t* ids_dev, float* weights_dev, int32_t* offsets_dev,
+                             int32_t* order_dev, int32_t* slot_dev, void* stream) {
+  if (!ctx || !logits_dev || !desc || !ids_dev || !weights_dev) return PSB_ERR_INVALID_ARG;
+  psb_route_desc d = *desc;
+  if (!is_real(d.in_dtype) || d.score > PSB_SCORE_SIGMOID || d.renormalise > 1u || !d.tokens || !d.experts || !d.top_k) return PSB_ERR_INVALID_ARG;
+  if (!d.groups || d.experts % d.groups || !d.top_groups || d.top_groups > d.groups || d.group_best < 1u || d.group_best > 2u)
+    return PSB_ERR_INVALID_ARG;
+  if ((uint64_t)d.top_k > (uint64_t)d.top_groups * (d.experts / d.groups)) return PSB_ERR_INVALID_ARG;
+  if (!offsets_dev != !order_dev || !offsets_dev != !slot_dev) return PSB_ERR_INVALID_ARG;
+  if (!row_stride(d.logit_stride, d.experts)) return PSB_ERR_INVALID_ARG;
+  if (misaligned(logits_dev, size_of(d.in_dtype)) || misaligned(bias_dev, 4) || misaligned(ids_dev, 4) || misaligned(weights_dev, 4) ||
+      misaligned(offsets_dev, 4) || misaligned(order_dev, 4) || misaligned(slot_dev, 4))
+    return PSB_ERR_INVALID_ARG;
+  if (d.experts > 1024u || d.top_k > 32u || (uint64_t)d.tokens * d.top_k >= (1ull << 31)) return PSB_ERR_UNSUPPORTED;
+  cudaSetDevice(ctx->device);
+  void* counts = nullptr;
+  if (order_dev) {
+    ScratchSet* sc = nullptr;
+    psb_status st = scratch_for(ctx, (cudaStream_t)stream, &sc);
+    if (st == PSB_OK) st = ensure_scratch(ctx, *sc, 4, route_scratch_bytes(d));
+    if (st != PSB_OK) return st;
+    counts = sc->buf[4];
+  }
+  return launch_route(logits_dev, bias_dev, token_mask_dev, d, ids_dev, weights_dev, offsets_dev, order_dev, slot_dev, counts,
+                      (cudaStream_t)stream) == cudaSuccess
+             ? PSB_OK
+             : PSB_ERR_CUDA;
+}
+
+psb_status psb_combine_experts(psb_ctx* ctx, const void* y_dev, const float* weights_dev, const int32_t* slot_dev,
+                               const psb_combine_desc* desc, void* out_dev, void* stream) {
+  if (!ctx || !y_dev || !weights_dev || !slot_dev || !desc || !out_dev) return PSB_ERR_INVALID_ARG;
+  psb_combine_desc d = *desc;
+  if (!is_real(d.in_dtype) || !is_real(d.out_dtype) || !d.tokens || !d.top_k || !d.n || !d.rows) return PSB_ERR_INVALID_ARG;
+  if (!row_stride(d.y_stride, d.n) || !row_stride(d.out_stride, d.n)) return PSB_ERR_INVALID_ARG;
+  if (misaligned(y_dev, size_of(d.in_dtype)) || misaligned(out_dev, size_of(d.out_dtype)) || misaligned(weights_dev, 4) || misaligned(slot_dev, 4))
+    return PSB_ERR_INVALID_ARG;
+  if (d.top_k > 32u || d.n >= (1u << 31) || d.rows >= (1u << 31) || (uint64_t)d.tokens * d.top_k >= (1ull << 31)) return PSB_ERR_UNSUPPORTED;
+  cudaSetDevice(ctx->device);
+  return launch_combine(y_dev, weights_dev, slot_dev, d, out_dev, ctx->err_dev, (cudaStream_t)stream) == cudaSuccess ? PSB_OK : PSB_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -85,7 +85,7 @@ struct psb_weights {
 
 // Work buffers of the calls on one stream: [0] layout conversion, [1] gathered activation matrix, [2] level-sorted
 // order of the current draw-count map (control block, permutation, tile levels), [3] activation rows in that
-// order.  Calls of one stream follow one another, so they share the buffers; calls of different streams may
+// order, [4] counts of the rows that go to each expert.  Calls of one stream follow one another, so they share the buffers; calls of different streams may
 // overlap and get their own.  Streams are told apart by their unique id: a handle is used again after a stream is
 // destroyed, and cudaStreamPerThread is one handle for a stream per thread.
 struct ScratchSet {
@@ -94,8 +94,8 @@ struct ScratchSet {
   unsigned long long last_use = 0;
   unsigned long long capture = 0;      // the capture that last used the set, 0 for eager calls
   bool in_graph = false;               // serves captured calls: the buffers stay until psb_destroy
-  void* buf[4] = {nullptr, nullptr, nullptr, nullptr};
-  size_t bytes[4] = {0, 0, 0, 0};
+  void* buf[5] = {nullptr, nullptr, nullptr, nullptr, nullptr};
+  size_t bytes[5] = {0, 0, 0, 0, 0};
   // the sorted order in buf[2] belongs to this map (pointer and dimensions); 0 rows = none
   const uint8_t* sorted_map = nullptr;
   uint32_t sorted_rows = 0;
@@ -294,6 +294,29 @@ cudaError_t launch_entropy(const void* act, uint32_t is_signed, uint32_t locatio
 cudaError_t launch_attention_maps(const float* entropy, uint32_t N, uint32_t H, uint32_t W, uint32_t lo_log2k,
                                   uint32_t hi_log2k, uint32_t n_res, const uint32_t* res, uint8_t* const* maps,
                                   float* mean_out, cudaStream_t s);
+
+// layers in 8-bit floating point (psb_quantize.cu, psb_fp8_gemm.cu); strides are never 0 here
+cudaError_t launch_quantize_fp8(const void* x, const psb_quantize_desc& d, uint8_t* codes, float* scales, cudaStream_t s);
+struct Fp8GemmArgs {
+  const uint8_t *a, *b;
+  const float *a_scale, *b_scale, *bias;
+  void* out;
+  uint32_t a_dtype, b_dtype, out_dtype;
+  uint32_t m, n, k, relu;     // m: rows of a
+  uint64_t a_stride, b_stride, a_scale_stride, b_scale_stride, out_stride;
+  // experts: 0 for one filter
+  uint32_t experts, rows;     // rows of out
+  uint64_t b_expert_stride, b_scale_expert_stride;
+  const int32_t *offsets, *order;
+};
+psb_status launch_gemm_fp8(psb_ctx* ctx, const Fp8GemmArgs& a, cudaStream_t s);
+
+// experts (psb_experts.cu); counts: scratch of route_scratch_bytes
+size_t route_scratch_bytes(const psb_route_desc& d);
+cudaError_t launch_route(const void* logits, const float* bias, const uint8_t* mask, const psb_route_desc& d, int32_t* ids,
+                         float* weights, int32_t* offsets, int32_t* order, int32_t* slot, void* counts, cudaStream_t s);
+cudaError_t launch_combine(const void* y, const float* weights, const int32_t* slot, const psb_combine_desc& d, void* out,
+                           uint32_t* err, cudaStream_t s);
 
 // int8 tensor-core issue-rate probe (psb_probe.cu)
 psb_status int8_mma_probe(psb_ctx* ctx, uint32_t n_cols, uint32_t groups, double* mac_per_clk_per_sm,

@@ -1,0 +1,509 @@
+// Routing of rows to experts, and the weighted sum of what the experts give back.
+//
+// route: a row's experts are those of the top_k largest select values.  Near the border two values may differ by less
+// than fp32 resolves, and a row sent to another expert is a wrong answer, so the comparison is exact: without a bias the
+// scores are monotone in the logits and the logits themselves are compared; otherwise fp32 values decide wherever
+// they are further apart than their error bound (kDoubt), and the row is done again in 64 bits where they are not (equal
+// logits with equal biases are equal, and need no second look).
+// The order of the choices is a counting sort: blocks of consecutive rows count their choices per expert; the
+// second launch adds up the counts of the blocks before it and places its own, the rank inside a block being the number of
+// earlier rows that chose the same expert (bit masks over the block's rows).  Nothing depends on the order of atomics.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "psb_common.cuh"
+
+namespace psb {
+
+namespace {
+
+constexpr uint32_t kAll = 0xFFFFFFFFu;
+constexpr uint32_t kRouteWarps = 8;
+constexpr uint32_t kMaxBlockRows = 1024;   // rows of a counting block: 32 words of a bit mask
+// Error of fp32 select values, relative to 1 + |value|: scores are at most 1 and their errors below 2e-6 (32 added terms a lane and five
+// of the tree, exp, quotient), the bias rounds once.  Two values are compared, hence twice.
+constexpr float kDoubt = 8e-6f;
+
+struct RouteArgs {
+  const void* logits;
+  const float* bias;
+  const uint8_t* mask;
+  uint32_t in_dtype, sigmoid, tokens, experts, top_k, groups, top_groups, group_best, renormalise;
+  float scaling;
+  uint64_t logit_stride;
+  int32_t *ids, *offsets, *order, *slot;
+  float* weights;
+  uint32_t* counts;        // [blocks][experts]
+  uint32_t block_rows, blocks;
+};
+
+// Monotone map of fp32 numbers onto words, 0 below all of them.
+__device__ __forceinline__ uint32_t key_of(float v) {
+  const uint32_t u = __float_as_uint(v);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t key) {
+  return __uint_as_float((key & 0x80000000u) ? (key & 0x7FFFFFFFu) : ~key);
+}
+__device__ __forceinline__ unsigned long long key_of(double v) {
+  const unsigned long long u = (unsigned long long)__double_as_longlong(v);
+  return (u >> 63) ? ~u : (u | (1ull << 63));
+}
+__device__ __forceinline__ double value_of(unsigned long long key) {
+  return __longlong_as_double((long long)((key >> 63) ? (key & ~(1ull << 63)) : ~key));
+}
+__device__ __forceinline__ uint32_t warp_max(uint32_t v) { return __reduce_max_sync(kAll, v); }
+__device__ __forceinline__ unsigned long long warp_max(unsigned long long v) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    const unsigned long long o = __shfl_xor_sync(kAll, v, d);
+    v = o > v ? o : v;
+  }
+  return v;
+}
+template <typename F> __device__ __forceinline__ F warp_sum(F v) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(kAll, v, d);
+  return v;
+}
+
+__device__ __forceinline__ float load_logit(const RouteArgs& a, uint64_t at) {
+  if (a.in_dtype == PSB_DT_F32) return ((const float*)a.logits)[at];
+  if (a.in_dtype == PSB_DT_BF16) return __bfloat162float(((const __nv_bfloat16*)a.logits)[at]);
+  return __half2float(((const __half*)a.logits)[at]);
+}
+
+template <typename F> struct KeyType;
+template <> struct KeyType<float> { typedef uint32_t type; };
+template <> struct KeyType<double> { typedef unsigned long long type; };
+
+template <typename F> __device__ __forceinline__ F exp_of(F x);
+template <> __device__ __forceinline__ float exp_of<float>(float x) { return __expf(x); }
+template <> __device__ __forceinline__ double exp_of<double>(double x) { return exp(x); }
+
+// The choices of one row, by a warp; lane l holds experts l, l + 32, ...  `x`: their logits, NaN where there is no such
+// expert or it is not available.  Lane j < top_k receives choice j (id -1: none) and its logit.  Returns whether the
+// comparisons were certain (F = double: always).
+template <typename F, int EL>
+__device__ __forceinline__ bool choose(const RouteArgs& a, const float (&x)[EL], float xmax, uint32_t lane, F* strength, int& my_id,
+                                       float& my_logit) {
+  typedef typename KeyType<F>::type Key;
+  const bool exact_type = sizeof(F) == 8;
+  const bool by_logit = !a.bias && a.groups == 1u;      // scores are monotone in the logits
+  Key key[EL];
+  bool sure = true;
+  if (by_logit) {
+#pragma unroll
+    for (int i = 0; i < EL; ++i) key[i] = x[i] == x[i] ? key_of((F)(x[i] + 0.0f)) : (Key)0;     // (-0 and 0 are equal)
+  } else {
+    F p[EL];
+    if (a.sigmoid) {
+#pragma unroll
+      for (int i = 0; i < EL; ++i) p[i] = (F)1 / ((F)1 + exp_of<F>(-(F)x[i]));
+    } else {
+      F sum = 0;
+#pragma unroll
+      for (int i = 0; i < EL; ++i) {
+        p[i] = exp_of<F>((F)x[i] - (F)xmax);
+        sum += x[i] == x[i] ? p[i] : (F)0;
+      }
+      sum = warp_sum(sum);
+      // (exactly: a quotient of the same two numbers for equal logits)
+#pragma unroll
+      for (int i = 0; i < EL; ++i) p[i] = p[i] / sum;
+    }
+#pragma unroll
+    for (int i = 0; i < EL; ++i) {
+      const uint32_t e = lane + 32u * i;
+      const F sel = p[i] + ((a.bias && e < a.experts) ? (F)__ldcg(a.bias + e) : (F)0);
+      key[i] = x[i] == x[i] && sel == sel ? key_of(sel + (F)0) : (Key)0;
+    }
+    if (a.groups > 1u) {
+      // strengths through shared memory: lane g takes groups g, g + 32, ...
+      Key* all = reinterpret_cast<Key*>(strength);           // [experts]
+      const uint32_t size = a.experts / a.groups;
+#pragma unroll
+      for (int i = 0; i < EL; ++i)
+        if (lane + 32u * i < a.experts) all[lane + 32u * i] = key[i];
+      __syncwarp();
+      Key* group = all + a.experts;                          // [groups]
+      F* size_of = reinterpret_cast<F*>(group + a.groups);   // [groups] magnitudes behind the strengths (fp32 alone)
+      for (uint32_t g = lane; g < a.groups; g += 32u) {
+        Key first = 0, second = 0;
+        for (uint32_t j = 0; j < size; ++j) {
+          const Key k = all[g * size + (j + lane) % size];
+          if (k > first) { second = first; first = k; }
+          else if (k > second) second = k;
+        }
+        const bool two = second && a.group_best > 1u;
+        group[g] = !first ? (Key)0 : key_of((two ? value_of(first) + value_of(second) : value_of(first)) + (F)0);
+        if (!exact_type) size_of[g] = (F)2 + (F)fabsf((float)value_of(first)) + (two ? (F)fabsf((float)value_of(second)) : (F)0);
+      }
+      __syncwarp();
+      // a group stays if fewer than top_groups are stronger, or as strong and before it
+      uint32_t stay = 0;       // bit i: my expert i stays
+      for (uint32_t g0 = 0; g0 < a.groups; g0 += 32u) {
+        const uint32_t g = g0 + lane;
+        const Key mine = g < a.groups ? group[g] : (Key)0;
+        uint32_t before = 0;
+        for (uint32_t o = 0; o < a.groups; ++o) {
+          const Key k = group[o];
+          before += (k > mine || (k == mine && o < g)) ? 1u : 0u;
+          if (!exact_type && g < a.groups && o != g && mine && k)
+            sure = sure && fabsf((float)value_of(k) - (float)value_of(mine)) > kDoubt * ((float)size_of[g] + (float)size_of[o]);
+        }
+        const uint32_t in = __ballot_sync(kAll, g < a.groups && before < a.top_groups);
+#pragma unroll
+        for (int i = 0; i < EL; ++i) {
+          const uint32_t mg = min(lane + 32u * i, a.experts - 1u) / size;
+          if (mg >= g0 && mg < g0 + 32u && ((in >> (mg - g0)) & 1u)) stay |= 1u << i;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < EL; ++i)
+        if (!((stay >> i) & 1u)) key[i] = 0;
+      __syncwarp();
+    }
+  }
+  my_id = -1;
+  my_logit = 0.0f;
+  Key last = 0;
+  float last_logit = 0.0f, last_bias = 0.0f;
+  // one round more than there are choices: is the last choice certain against the first that is left out
+  const uint32_t rounds = a.top_k + (exact_type || by_logit ? 0u : 1u);
+  for (uint32_t j = 0; j < rounds; ++j) {
+    Key best = 0;
+    uint32_t at = 0;
+    float logit = 0.0f;
+#pragma unroll
+    for (int i = 0; i < EL; ++i)
+      if (key[i] > best) { best = key[i]; at = (uint32_t)i; logit = x[i]; }
+    const Key top = warp_max(best);
+    if (!top) break;
+    const uint32_t id = __reduce_min_sync(kAll, best == top ? at * 32u + lane : 0xFFFFFFFFu);
+    const float id_logit = __shfl_sync(kAll, logit, (int)(id & 31u));
+    if (!exact_type && !by_logit) {
+      const float id_bias = a.bias ? __ldcg(a.bias + id) : 0.0f;
+      if (j > 0u) {
+        const float v = (float)value_of(top), gap = (float)value_of(last) - v;
+        sure = sure && (gap > kDoubt * (1.0f + fabsf(v)) || (id_logit == last_logit && id_bias == last_bias));
+      }
+      last_logit = id_logit;
+      last_bias = id_bias;
+    }
+    last = top;
+    if (lane == j && j < a.top_k) { my_id = (int)id; my_logit = id_logit; }
+    if (lane == (id & 31u)) {
+#pragma unroll
+      for (int i = 0; i < EL; ++i)
+        if ((uint32_t)i == (id >> 5)) key[i] = 0;
+    }
+  }
+  return __all_sync(kAll, sure);
+}
+
+// Rows of a block one after another by its warps.  Dynamic shared memory: counts [experts], then per warp the group scratch.
+template <int EL>
+__global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs a) {
+  pdl_prologue();
+  extern __shared__ unsigned char route_smem[];
+  uint32_t* hist = reinterpret_cast<uint32_t*>(route_smem);
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  double* scratch = reinterpret_cast<double*>(route_smem + ((a.experts * 4u + 15u) & ~15u)) + (size_t)warp * (a.experts + a.groups);
+  for (uint32_t e = threadIdx.x; e < a.experts; e += blockDim.x) hist[e] = 0u;
+  __syncthreads();
+  const uint32_t lo = blockIdx.x * a.block_rows, hi = min(lo + a.block_rows, a.tokens);
+  for (uint32_t t = lo + warp; t < hi; t += kRouteWarps) {
+    const bool on = !a.mask || a.mask[t] != 0u;
+    int id = -1;
+    float logit = 0.0f, w = 0.0f;
+    if (on) {
+      float x[EL];
+      float m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < EL; ++i) {
+        const uint32_t e = lane + 32u * i;
+        float v = e < a.experts ? load_logit(a, t * a.logit_stride + e) : NAN;
+        if (v == INFINITY) v = 3.402823466e38f;
+        if (v == -INFINITY) v = NAN;
+        x[i] = v;
+        m = fmaxf(m, v);                  // (NaN counts as absent)
+      }
+      m = value_of(warp_max(key_of(m)));
+      if (!choose<float, EL>(a, x, m, lane, reinterpret_cast<float*>(scratch), id, logit))
+        choose<double, EL>(a, x, m, lane, scratch, id, logit);
+      const bool mine = id >= 0;
+      float s = 0.0f;
+      if (a.renormalise) {
+        // ratios of scores, without under- or overflow: softmax exp(x - top) and sigmoid
+        // exp(min(x, 0) - min(top, 0)) / (1 + exp(-|x|)) up to factors that the choices share
+        const float top = value_of(warp_max(mine ? key_of(logit) : 0u));
+        if (mine) s = a.sigmoid ? expf(fminf(logit, 0.0f) - fminf(top, 0.0f)) / (1.0f + expf(-fabsf(logit))) : expf(logit - top);
+        const float sum = warp_sum(s);
+        s = mine ? s / sum : 0.0f;
+      } else if (a.sigmoid) {
+        s = mine ? (logit >= 0.0f ? 1.0f / (1.0f + expf(-logit)) : expf(logit) / (1.0f + expf(logit))) : 0.0f;
+      } else {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < EL; ++i) sum += x[i] == x[i] ? expf(x[i] - m) : 0.0f;
+        sum = warp_sum(sum);
+        s = mine ? expf(logit - m) / sum : 0.0f;
+      }
+      w = s * a.scaling;
+    }
+    if (lane < a.top_k) {
+      a.ids[(size_t)t * a.top_k + lane] = id;
+      a.weights[(size_t)t * a.top_k + lane] = id >= 0 ? w : 0.0f;
+      if (id >= 0) atomicAdd(&hist[id], 1u);
+    }
+  }
+  if (!a.counts) return;
+  __syncthreads();
+  for (uint32_t e = threadIdx.x; e < a.experts; e += blockDim.x) a.counts[(size_t)blockIdx.x * a.experts + e] = hist[e];
+}
+
+// Places the choices of each block.  Dynamic shared memory: places [experts] and, per expert, a bit for each row of
+// the block.
+__global__ void __launch_bounds__(512) order_kernel(const RouteArgs a) {
+  pdl_prologue();
+  extern __shared__ uint32_t order_smem[];
+  uint32_t *place = order_smem, *bits = order_smem + a.experts;
+  __shared__ uint32_t warp_total[16];
+  const uint32_t words = a.block_rows / 32u, lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  const uint32_t lo = blockIdx.x * a.block_rows, hi = min(lo + a.block_rows, a.tokens), choices = (hi - lo) * a.top_k;
+  for (uint32_t i = threadIdx.x; i < a.experts * words; i += blockDim.x) bits[i] = 0u;
+  // how many rows of all blocks, and of the blocks before this one, go to each expert; the first place of each expert
+  uint32_t carry = 0;
+  for (uint32_t e0 = 0; e0 < a.experts; e0 += blockDim.x) {
+    const uint32_t e = e0 + threadIdx.x;
+    uint32_t all = 0, before = 0;
+    if (e < a.experts) {
+#pragma unroll 8
+      for (uint32_t b = 0; b < a.blocks; ++b) {
+        const uint32_t c = __ldcg(a.counts + (size_t)b * a.experts + e);
+        all += c;
+        before += b < blockIdx.x ? c : 0u;
+      }
+    }
+    uint32_t up = all;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const uint32_t o = __shfl_up_sync(kAll, up, d);
+      if (lane >= (uint32_t)d) up += o;
+    }
+    if (lane == 31u) warp_total[warp] = up;
+    __syncthreads();
+    uint32_t base = carry, total = 0;
+    for (uint32_t w = 0; w < blockDim.x / 32u; ++w) {
+      if (w < warp) base += warp_total[w];
+      total += warp_total[w];
+    }
+    if (e < a.experts) {
+      place[e] = base + up - all + before;
+      if (blockIdx.x == 0u) a.offsets[e] = (int32_t)(base + up - all);
+    }
+    carry += total;
+    __syncthreads();
+  }
+  if (blockIdx.x == 0u && threadIdx.x == 0u) a.offsets[a.experts] = (int32_t)carry;
+  for (uint32_t i = threadIdx.x; i < choices; i += blockDim.x) {
+    const int id = __ldcg(a.ids + (size_t)lo * a.top_k + i);
+    const uint32_t r = i / a.top_k;
+    if (id >= 0) atomicOr(&bits[(uint32_t)id * words + r / 32u], 1u << (r & 31u));
+  }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < choices; i += blockDim.x) {
+    const int id = __ldcg(a.ids + (size_t)lo * a.top_k + i);
+    const uint32_t r = i / a.top_k;
+    int at = -1;
+    if (id >= 0) {
+      uint32_t rank = __popc(bits[(uint32_t)id * words + r / 32u] & ((1u << (r & 31u)) - 1u));
+      for (uint32_t w = 0; w < r / 32u; ++w) rank += __popc(bits[(uint32_t)id * words + w]);
+      at = (int)(place[id] + rank);
+      a.order[at] = (int32_t)(lo + r);
+    }
+    a.slot[(size_t)lo * a.top_k + i] = at;
+  }
+  // behind the last
+  const uint64_t end = (uint64_t)a.tokens * a.top_k;
+  for (uint64_t i = carry + (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < end; i += (uint64_t)gridDim.x * blockDim.x) a.order[i] = -1;
+}
+
+uint32_t rows_of_a_block(const psb_route_desc& d) {
+  // a block per SM, in whole words of the bit masks
+  uint32_t rows = round_up((d.tokens + kSms - 1u) / kSms, 32u);
+  return rows < kMaxBlockRows ? rows : kMaxBlockRows;
+}
+
+// ---- combine -------------------------------------------------------------------------------------------------------------
+
+template <typename T> __device__ __forceinline__ float as_f32(T v);
+template <> __device__ __forceinline__ float as_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ float as_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float as_f32<__half>(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+
+struct CombineArgs {
+  const void* y;
+  const float* weights;
+  const int32_t* slot;
+  void* out;
+  uint32_t* err;
+  uint32_t tokens, top_k, n, rows, chunks, wide;   // chunks: pieces of 16 input bytes in a row
+  uint64_t y_stride, out_stride;
+};
+
+// A thread owns 16 input bytes of an output row; the rows of up to eight choices are loaded together.
+template <typename TI, typename TO>
+__global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a) {
+  pdl_prologue();
+  constexpr int kPer = 16 / sizeof(TI);
+  const uint64_t total = (uint64_t)a.tokens * a.chunks;
+  for (uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (uint64_t)gridDim.x * blockDim.x) {
+    const uint32_t t = (uint32_t)(i / a.chunks), c = (uint32_t)(i - (uint64_t)t * a.chunks) * kPer;
+    const bool whole = a.wide && c + kPer <= a.n;
+    float sum[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) sum[e] = 0.0f;
+    for (uint32_t j0 = 0; j0 < a.top_k; j0 += 8u) {
+      uint4 v[8];
+      float w[8];
+      bool on[8];
+#pragma unroll
+      for (uint32_t j = 0; j < 8u; ++j) {
+        const bool there = j0 + j < a.top_k;
+        const int s = there ? a.slot[(size_t)t * a.top_k + j0 + j] : -1;
+        if (s >= 0 && (uint32_t)s >= a.rows) atomicOr(a.err, kDevErrRange);
+        on[j] = s >= 0 && (uint32_t)s < a.rows;
+        w[j] = on[j] ? a.weights[(size_t)t * a.top_k + j0 + j] : 0.0f;
+        const TI* row = (const TI*)a.y + (on[j] ? (uint64_t)s : 0u) * a.y_stride + c;
+        if (whole) {
+          if (on[j]) v[j] = *reinterpret_cast<const uint4*>(row);
+        } else {
+          TI* parts = reinterpret_cast<TI*>(&v[j]);
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) parts[e] = on[j] && c + e < a.n ? row[e] : from_f32<TI>(0.0f);
+        }
+      }
+#pragma unroll
+      for (uint32_t j = 0; j < 8u; ++j) {
+        if (!on[j]) continue;
+        const TI* parts = reinterpret_cast<const TI*>(&v[j]);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) sum[e] = __fmaf_rn(w[j], as_f32<TI>(parts[e]), sum[e]);
+      }
+    }
+    TO* out = (TO*)a.out + t * a.out_stride + c;
+    if (whole) {
+      constexpr int kBytes = kPer * (int)sizeof(TO);      // 8, 16 or 32
+      alignas(16) TO parts[kPer];
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) parts[e] = from_f32<TO>(sum[e]);
+      if (kBytes == 8) {
+        *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(parts);
+      } else {
+#pragma unroll
+        for (int b = 0; b < kBytes / 16; ++b) reinterpret_cast<uint4*>(out)[b] = reinterpret_cast<const uint4*>(parts)[b];
+      }
+    } else {
+      for (int e = 0; e < kPer; ++e)
+        if (c + e < a.n) out[e] = from_f32<TO>(sum[e]);
+    }
+  }
+}
+
+template <typename TI, typename TO>
+void launch_combine_as(const CombineArgs& a, cudaStream_t s) {
+  const uint64_t want = ((uint64_t)a.tokens * a.chunks + 255u) / 256u;
+  launch_pdl(combine_kernel<TI, TO>, (uint32_t)(want < kSms * 64u ? want : kSms * 64u), 256, 0, s, a);
+}
+template <typename TI>
+void launch_combine_from(const CombineArgs& a, uint32_t out_dtype, cudaStream_t s) {
+  if (out_dtype == PSB_DT_F32) launch_combine_as<TI, float>(a, s);
+  else if (out_dtype == PSB_DT_BF16) launch_combine_as<TI, __nv_bfloat16>(a, s);
+  else launch_combine_as<TI, __half>(a, s);
+}
+
+}  // namespace
+
+size_t route_scratch_bytes(const psb_route_desc& d) {
+  const uint32_t rows = rows_of_a_block(d);
+  return (size_t)((d.tokens + rows - 1u) / rows) * d.experts * sizeof(uint32_t);
+}
+
+cudaError_t launch_route(const void* logits, const float* bias, const uint8_t* mask, const psb_route_desc& d, int32_t* ids,
+                         float* weights, int32_t* offsets, int32_t* order, int32_t* slot, void* counts, cudaStream_t s) {
+  RouteArgs a;
+  a.logits = logits;
+  a.bias = bias;
+  a.mask = mask;
+  a.in_dtype = d.in_dtype;
+  a.sigmoid = d.score == PSB_SCORE_SIGMOID;
+  a.tokens = d.tokens;
+  a.experts = d.experts;
+  a.top_k = d.top_k;
+  a.groups = d.groups;
+  a.top_groups = d.top_groups;
+  a.group_best = d.group_best;
+  a.renormalise = d.renormalise;
+  a.scaling = d.scaling;
+  a.logit_stride = d.logit_stride;
+  a.ids = ids;
+  a.weights = weights;
+  a.offsets = offsets;
+  a.order = order;
+  a.slot = slot;
+  a.counts = order ? (uint32_t*)counts : nullptr;
+  a.block_rows = rows_of_a_block(d);
+  a.blocks = (d.tokens + a.block_rows - 1u) / a.block_rows;
+  const size_t smem = ((d.experts * 4u + 15u) & ~15u) + (d.groups > 1u ? sizeof(double) * kRouteWarps * (d.experts + d.groups) : 0u);
+  const uint32_t per_lane = (d.experts + 31u) / 32u;
+  auto go = [&](auto kernel) {
+    if (smem > 48u * 1024u) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    launch_pdl(kernel, a.blocks, kRouteWarps * 32u, smem, s, a);
+  };
+  if (per_lane <= 1u) go(route_kernel<1>);
+  else if (per_lane <= 2u) go(route_kernel<2>);
+  else if (per_lane <= 4u) go(route_kernel<4>);
+  else if (per_lane <= 8u) go(route_kernel<8>);
+  else if (per_lane <= 16u) go(route_kernel<16>);
+  else go(route_kernel<32>);
+  note_launch();
+  if (order) {
+    const size_t bytes = sizeof(uint32_t) * d.experts * (1u + a.block_rows / 32u);
+    if (bytes > 48u * 1024u) cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    launch_pdl(order_kernel, a.blocks, 512, bytes, s, a);
+    note_launch();
+  }
+  return cudaGetLastError();
+}
+
+cudaError_t launch_combine(const void* y, const float* weights, const int32_t* slot, const psb_combine_desc& d, void* out,
+                           uint32_t* err, cudaStream_t s) {
+  CombineArgs a;
+  a.y = y;
+  a.weights = weights;
+  a.slot = slot;
+  a.out = out;
+  a.err = err;
+  a.tokens = d.tokens;
+  a.top_k = d.top_k;
+  a.n = d.n;
+  a.rows = d.rows;
+  a.y_stride = d.y_stride;
+  a.out_stride = d.out_stride;
+  const uint32_t in = d.in_dtype == PSB_DT_F32 ? 4u : 2u, to = d.out_dtype == PSB_DT_F32 ? 4u : 2u;
+  a.chunks = (d.n + 16u / in - 1u) / (16u / in);
+  a.wide = (((uintptr_t)y | (uintptr_t)out | d.y_stride * in | d.out_stride * to) & 15u) == 0u;
+  if (d.in_dtype == PSB_DT_F32) launch_combine_from<float>(a, d.out_dtype, s);
+  else if (d.in_dtype == PSB_DT_BF16) launch_combine_from<__nv_bfloat16>(a, d.out_dtype, s);
+  else launch_combine_from<__half>(a, d.out_dtype, s);
+  note_launch();
+  return cudaGetLastError();
+}
+
+}  // namespace psb
