@@ -415,8 +415,9 @@ psb_status psb_sample_level_static(const float* w_dev, const psb_wshape* shape,
  *
  * Conventions of these five calls: matrices are row-major, elements of a row follow one another, rows are `*_stride`
  * elements apart (0: as many as a row has; blocks of a scale row likewise).  Strides may exceed the row; what
- * lies between rows is neither read nor written.  Nothing is allocated except by psb_route_experts (scratch, see the
- * top of this file).  They run on the context's device, which becomes the current one. */
+ * lies between rows is neither read nor written.  Scratch is taken by psb_route_experts (counts) and, with an order, by
+ * psb_gemm_fp8_experts (the rows in that order), see the
+ * top of this file.  They run on the context's device, which becomes the current one. */
 
 /* Codes and scales of a matrix.  Per block of block_rows x 128 (1: activations, 128: filters; blocks at the ends are
  * cut off):

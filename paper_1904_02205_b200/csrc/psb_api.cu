@@ -813,7 +813,7 @@ psb_status psb_gemm_fp8(psb_ctx* ctx, const uint8_t* a_dev, const float* a_scale
   const psb_status st = check_gemm_fp8(a_dev, a_scale_dev, b_dev, b_scale_dev, out_dev, *desc, g);
   if (st != PSB_OK) return st;
   cudaSetDevice(ctx->device);
-  return launch_gemm_fp8(ctx, g, (cudaStream_t)stream);
+  return launch_gemm_fp8(ctx, g, nullptr, (cudaStream_t)stream);
 }
 
 psb_status psb_gemm_fp8_experts(psb_ctx* ctx, const uint8_t* a_dev, const float* a_scale_dev, const uint8_t* b_dev,
@@ -837,7 +837,15 @@ psb_status psb_gemm_fp8_experts(psb_ctx* ctx, const uint8_t* a_dev, const float*
   g.offsets = offsets_dev;
   g.order = order_dev;
   cudaSetDevice(ctx->device);
-  return launch_gemm_fp8(ctx, g, (cudaStream_t)stream);
+  void* scratch = nullptr;
+  if (order_dev) {
+    ScratchSet* sc = nullptr;
+    psb_status found = scratch_for(ctx, (cudaStream_t)stream, &sc);
+    if (found == PSB_OK) found = ensure_scratch(ctx, *sc, 1, gemm_fp8_scratch_bytes(g));
+    if (found != PSB_OK) return found;
+    scratch = sc->buf[1];
+  }
+  return launch_gemm_fp8(ctx, g, scratch, (cudaStream_t)stream);
 }
 
 psb_status psb_route_experts(psb_ctx* ctx, const void* logits_dev, const float* bias_dev, const uint8_t* token_mask_dev,

@@ -309,7 +309,8 @@ struct Fp8GemmArgs {
   uint64_t b_expert_stride, b_scale_expert_stride;
   const int32_t *offsets, *order;
 };
-psb_status launch_gemm_fp8(psb_ctx* ctx, const Fp8GemmArgs& a, cudaStream_t s);
+size_t gemm_fp8_scratch_bytes(const Fp8GemmArgs& a);
+psb_status launch_gemm_fp8(psb_ctx* ctx, const Fp8GemmArgs& a, void* scratch, cudaStream_t s);
 
 // experts (psb_experts.cu); counts: scratch of route_scratch_bytes
 size_t route_scratch_bytes(const psb_route_desc& d);

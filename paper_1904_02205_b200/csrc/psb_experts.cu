@@ -18,7 +18,7 @@ namespace psb {
 namespace {
 
 constexpr uint32_t kAll = 0xFFFFFFFFu;
-constexpr uint32_t kRouteWarps = 8;
+template <int EL> constexpr uint32_t kRouteThreads = EL <= 8 ? 512u : 256u;
 constexpr uint32_t kMaxBlockRows = 1024;   // rows of a counting block: 32 words of a bit mask
 // Error of fp32 select values, relative to 1 + |value|: scores are at most 1 and their errors below 2e-6 (32 added terms a lane and five
 // of the tree, exp, quotient), the bias rounds once.  Two values are compared, hence twice.
@@ -35,6 +35,10 @@ struct RouteArgs {
   float* weights;
   uint32_t* counts;        // [blocks][experts]
   uint32_t block_rows, blocks;
+  uint32_t alone;            // one block has all rows and places them itself
+  uint32_t wide;             // rows of logits start at multiples of 16 bytes
+  uint32_t lanes_per_group;  // a power of two where groups are the experts of whole lanes, else 0
+  uint32_t share;            // threads that add up the counts of an expert
 };
 
 // Monotone map of fp32 numbers onto words, 0 below all of them.
@@ -73,6 +77,9 @@ __device__ __forceinline__ float load_logit(const RouteArgs& a, uint64_t at) {
   return __half2float(((const __half*)a.logits)[at]);
 }
 
+__device__ __forceinline__ float quotient(float p, float q) { return __fdividef(p, q); }      // 2 ulp
+__device__ __forceinline__ double quotient(double p, double q) { return p / q; }
+
 template <typename F> struct KeyType;
 template <> struct KeyType<float> { typedef uint32_t type; };
 template <> struct KeyType<double> { typedef unsigned long long type; };
@@ -81,12 +88,61 @@ template <typename F> __device__ __forceinline__ F exp_of(F x);
 template <> __device__ __forceinline__ float exp_of<float>(float x) { return __expf(x); }
 template <> __device__ __forceinline__ double exp_of<double>(double x) { return exp(x); }
 
-// The choices of one row, by a warp; lane l holds experts l, l + 32, ...  `x`: their logits, NaN where there is no such
-// expert or it is not available.  Lane j < top_k receives choice j (id -1: none) and its logit.  Returns whether the
-// comparisons were certain (F = double: always).
+// The lane's logits, experts lane * EL ...; NaN where there is no such expert or it is not available.
+template <int EL>
+__device__ __forceinline__ void load_logits(const RouteArgs& a, uint32_t t, uint32_t lane, float (&x)[EL]) {
+  const uint32_t e0 = lane * EL;
+  const uint64_t at = (uint64_t)t * a.logit_stride + e0;
+  const bool whole = e0 + EL <= a.experts;
+  if (EL >= 4 && a.wide && whole && a.in_dtype == PSB_DT_F32) {
+#pragma unroll
+    for (int i = 0; i < EL / 4; ++i) {
+      const float4 w = *reinterpret_cast<const float4*>((const float*)a.logits + at + 4 * i);
+      x[4 * i] = w.x;
+      x[4 * i + 1] = w.y;
+      x[(4 * i + 2) % EL] = w.z;
+      x[(4 * i + 3) % EL] = w.w;
+    }
+  } else if (EL >= 4 && a.wide && whole) {
+#pragma unroll
+    for (int i = 0; i < EL / 4; ++i) {
+      const uint2 w = *reinterpret_cast<const uint2*>((const uint16_t*)a.logits + at + 4 * i);
+      const uint32_t h[4] = {w.x & 0xFFFFu, w.x >> 16, w.y & 0xFFFFu, w.y >> 16};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        x[(4 * i + j) % EL] = a.in_dtype == PSB_DT_BF16 ? __uint_as_float(h[j] << 16) : __half2float(__ushort_as_half((uint16_t)h[j]));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < EL; ++i) x[i] = e0 + i < a.experts ? load_logit(a, at + i) : NAN;
+  }
+#pragma unroll
+  for (int i = 0; i < EL; ++i) {
+    if (x[i] == INFINITY) x[i] = 3.402823466e38f;
+    if (x[i] == -INFINITY) x[i] = NAN;
+  }
+}
+
+// Whether two experts of a row have the same logit and the same bias (a look at memory: the registers are another lane's).
+__device__ __noinline__ bool same_select(const RouteArgs& a, uint32_t t, uint32_t e, uint32_t o) {
+  return load_logit(a, (uint64_t)t * a.logit_stride + e) == load_logit(a, (uint64_t)t * a.logit_stride + o) &&
+         (!a.bias || __ldcg(a.bias + e) == __ldcg(a.bias + o));
+}
+
+// The two largest keys of a run of experts, put together with those of another run.
+template <typename Key>
+__device__ __forceinline__ void merge_best(Key& first, Key& second, Key f, Key s) {
+  const Key low = f < first ? f : first;
+  first = f > first ? f : first;
+  second = s > second ? s : second;
+  second = low > second ? low : second;
+}
+
+// The choices of one row, by a warp; lane l holds experts l * EL ...  Lane j < top_k receives choice j (id -1: none)
+// and its logit.  Returns whether the comparisons were certain (F = double: always).
 template <typename F, int EL>
-__device__ __forceinline__ bool choose(const RouteArgs& a, const float (&x)[EL], float xmax, uint32_t lane, F* strength, int& my_id,
-                                       float& my_logit) {
+__device__ __forceinline__ bool choose(const RouteArgs& a, const float (&x)[EL], const float (&bias)[EL], float xmax, uint32_t t,
+                                       uint32_t lane, F* strength, int& my_id, float& my_logit) {
   typedef typename KeyType<F>::type Key;
   const bool exact_type = sizeof(F) == 8;
   const bool by_logit = !a.bias && a.groups == 1u;      // scores are monotone in the logits
@@ -99,7 +155,7 @@ __device__ __forceinline__ bool choose(const RouteArgs& a, const float (&x)[EL],
     F p[EL];
     if (a.sigmoid) {
 #pragma unroll
-      for (int i = 0; i < EL; ++i) p[i] = (F)1 / ((F)1 + exp_of<F>(-(F)x[i]));
+      for (int i = 0; i < EL; ++i) p[i] = quotient((F)1, (F)1 + exp_of<F>(-(F)x[i]));
     } else {
       F sum = 0;
 #pragma unroll
@@ -108,205 +164,179 @@ __device__ __forceinline__ bool choose(const RouteArgs& a, const float (&x)[EL],
         sum += x[i] == x[i] ? p[i] : (F)0;
       }
       sum = warp_sum(sum);
-      // (exactly: a quotient of the same two numbers for equal logits)
 #pragma unroll
-      for (int i = 0; i < EL; ++i) p[i] = p[i] / sum;
+      for (int i = 0; i < EL; ++i) p[i] = quotient(p[i], sum);
     }
 #pragma unroll
     for (int i = 0; i < EL; ++i) {
-      const uint32_t e = lane + 32u * i;
-      const F sel = p[i] + ((a.bias && e < a.experts) ? (F)__ldcg(a.bias + e) : (F)0);
+      const F sel = p[i] + (F)bias[i];
       key[i] = x[i] == x[i] && sel == sel ? key_of(sel + (F)0) : (Key)0;
     }
     if (a.groups > 1u) {
-      // strengths through shared memory: lane g takes groups g, g + 32, ...
-      Key* all = reinterpret_cast<Key*>(strength);           // [experts]
       const uint32_t size = a.experts / a.groups;
-#pragma unroll
-      for (int i = 0; i < EL; ++i)
-        if (lane + 32u * i < a.experts) all[lane + 32u * i] = key[i];
-      __syncwarp();
-      Key* group = all + a.experts;                          // [groups]
-      F* size_of = reinterpret_cast<F*>(group + a.groups);   // [groups] magnitudes behind the strengths (fp32 alone)
-      for (uint32_t g = lane; g < a.groups; g += 32u) {
+      uint32_t stay = 0;       // bit i: my expert i stays
+      if (a.lanes_per_group) {
+        // a group is the experts of 1, 2, 4 ... lanes: every lane learns its group's strength
         Key first = 0, second = 0;
-        for (uint32_t j = 0; j < size; ++j) {
-          const Key k = all[g * size + (j + lane) % size];
-          if (k > first) { second = first; first = k; }
-          else if (k > second) second = k;
+#pragma unroll
+        for (int i = 0; i < EL; ++i) merge_best(first, second, key[i], (Key)0);
+        for (uint32_t d = 1; d < a.lanes_per_group; d <<= 1) {
+          const Key f = __shfl_xor_sync(kAll, first, (int)d), s = __shfl_xor_sync(kAll, second, (int)d);
+          merge_best(first, second, f, s);
         }
         const bool two = second && a.group_best > 1u;
-        group[g] = !first ? (Key)0 : key_of((two ? value_of(first) + value_of(second) : value_of(first)) + (F)0);
-        if (!exact_type) size_of[g] = (F)2 + (F)fabsf((float)value_of(first)) + (two ? (F)fabsf((float)value_of(second)) : (F)0);
-      }
-      __syncwarp();
-      // a group stays if fewer than top_groups are stronger, or as strong and before it
-      uint32_t stay = 0;       // bit i: my expert i stays
-      for (uint32_t g0 = 0; g0 < a.groups; g0 += 32u) {
-        const uint32_t g = g0 + lane;
-        const Key mine = g < a.groups ? group[g] : (Key)0;
+        const Key mine = !first ? (Key)0 : key_of((two ? value_of(first) + value_of(second) : value_of(first)) + (F)0);
+        const float far = exact_type ? 0.0f : kDoubt * (2.0f + fabsf((float)value_of(first)) + (two ? fabsf((float)value_of(second)) : 0.0f));
         uint32_t before = 0;
-        for (uint32_t o = 0; o < a.groups; ++o) {
-          const Key k = group[o];
-          before += (k > mine || (k == mine && o < g)) ? 1u : 0u;
-          if (!exact_type && g < a.groups && o != g && mine && k)
-            sure = sure && fabsf((float)value_of(k) - (float)value_of(mine)) > kDoubt * ((float)size_of[g] + (float)size_of[o]);
+        for (uint32_t g = 0; g < a.groups; ++g) {
+          const uint32_t from = g * a.lanes_per_group;
+          const Key k = __shfl_sync(kAll, mine, (int)from);
+          before += (k > mine || (k == mine && from < (lane & ~(a.lanes_per_group - 1u)))) ? 1u : 0u;
+          if (!exact_type) {
+            const float doubt = far + __shfl_sync(kAll, far, (int)from);
+            if (mine && k && from != (lane & ~(a.lanes_per_group - 1u)))
+              sure = sure && fabsf((float)value_of(k) - (float)value_of(mine)) > doubt;
+          }
         }
-        const uint32_t in = __ballot_sync(kAll, g < a.groups && before < a.top_groups);
+        stay = before < a.top_groups ? 0xFFFFFFFFu : 0u;
+        sure = sure || lane >= a.groups * a.lanes_per_group;
+      } else {
+        // strengths through shared memory: lane g takes groups g, g + 32, ...
+        Key* all = reinterpret_cast<Key*>(strength);           // [experts]
 #pragma unroll
-        for (int i = 0; i < EL; ++i) {
-          const uint32_t mg = min(lane + 32u * i, a.experts - 1u) / size;
-          if (mg >= g0 && mg < g0 + 32u && ((in >> (mg - g0)) & 1u)) stay |= 1u << i;
+        for (int i = 0; i < EL; ++i)
+          if (lane * EL + i < a.experts) all[lane * EL + i] = key[i];
+        __syncwarp();
+        Key* group = all + a.experts;                          // [groups]
+        F* size_of = reinterpret_cast<F*>(group + a.groups);   // [groups] magnitudes behind the strengths (fp32 alone)
+        for (uint32_t g = lane; g < a.groups; g += 32u) {
+          Key first = 0, second = 0;
+          for (uint32_t j = 0; j < size; ++j) merge_best(first, second, all[g * size + j], (Key)0);
+          const bool two = second && a.group_best > 1u;
+          group[g] = !first ? (Key)0 : key_of((two ? value_of(first) + value_of(second) : value_of(first)) + (F)0);
+          if (!exact_type) size_of[g] = (F)2 + (F)fabsf((float)value_of(first)) + (two ? (F)fabsf((float)value_of(second)) : (F)0);
         }
+        __syncwarp();
+        // a group stays if fewer than top_groups are stronger, or as strong and before it
+        for (uint32_t g0 = 0; g0 < a.groups; g0 += 32u) {
+          const uint32_t g = g0 + lane;
+          const Key mine = g < a.groups ? group[g] : (Key)0;
+          uint32_t before = 0;
+          for (uint32_t o = 0; o < a.groups; ++o) {
+            const Key k = group[o];
+            before += (k > mine || (k == mine && o < g)) ? 1u : 0u;
+            if (!exact_type && g < a.groups && o != g && mine && k)
+              sure = sure && fabsf((float)value_of(k) - (float)value_of(mine)) > kDoubt * ((float)size_of[g] + (float)size_of[o]);
+          }
+          const uint32_t in = __ballot_sync(kAll, g < a.groups && before < a.top_groups);
+#pragma unroll
+          for (int i = 0; i < EL; ++i) {
+            const uint32_t mg = min(lane * EL + i, a.experts - 1u) / size;
+            if (mg >= g0 && mg < g0 + 32u && ((in >> (mg - g0)) & 1u)) stay |= 1u << i;
+          }
+        }
+        __syncwarp();
       }
 #pragma unroll
       for (int i = 0; i < EL; ++i)
         if (!((stay >> i) & 1u)) key[i] = 0;
-      __syncwarp();
     }
   }
   my_id = -1;
   my_logit = 0.0f;
+  // the lane's best, found again only where it has been taken
+  Key best = 0;
+  uint32_t at = 0;
+#pragma unroll
+  for (int i = 0; i < EL; ++i)
+    if (key[i] > best) { best = key[i]; at = (uint32_t)i; }
   Key last = 0;
-  float last_logit = 0.0f, last_bias = 0.0f;
+  uint32_t last_id = 0;
   // one round more than there are choices: is the last choice certain against the first that is left out
   const uint32_t rounds = a.top_k + (exact_type || by_logit ? 0u : 1u);
   for (uint32_t j = 0; j < rounds; ++j) {
-    Key best = 0;
-    uint32_t at = 0;
-    float logit = 0.0f;
-#pragma unroll
-    for (int i = 0; i < EL; ++i)
-      if (key[i] > best) { best = key[i]; at = (uint32_t)i; logit = x[i]; }
     const Key top = warp_max(best);
     if (!top) break;
-    const uint32_t id = __reduce_min_sync(kAll, best == top ? at * 32u + lane : 0xFFFFFFFFu);
-    const float id_logit = __shfl_sync(kAll, logit, (int)(id & 31u));
-    if (!exact_type && !by_logit) {
-      const float id_bias = a.bias ? __ldcg(a.bias + id) : 0.0f;
-      if (j > 0u) {
-        const float v = (float)value_of(top), gap = (float)value_of(last) - v;
-        sure = sure && (gap > kDoubt * (1.0f + fabsf(v)) || (id_logit == last_logit && id_bias == last_bias));
-      }
-      last_logit = id_logit;
-      last_bias = id_bias;
+    const uint32_t from = (uint32_t)__ffs((int)__ballot_sync(kAll, best == top)) - 1u;     // the lowest lane, the lowest expert
+    const uint32_t id = from * EL + __shfl_sync(kAll, at, (int)from);
+    if (!exact_type && !by_logit && j > 0u) {
+      const float v = (float)value_of(top), gap = (float)value_of(last) - v;
+      // (equal logits under equal biases are equal)
+      if (!(gap > kDoubt * (1.0f + fabsf(v)))) sure = sure && same_select(a, t, id, last_id);
     }
     last = top;
-    if (lane == j && j < a.top_k) { my_id = (int)id; my_logit = id_logit; }
-    if (lane == (id & 31u)) {
+    last_id = id;
+    if (j < a.top_k && lane == j) my_id = (int)id;
+    if (lane == from) {
+      best = 0;
+      const uint32_t gone = at;
 #pragma unroll
-      for (int i = 0; i < EL; ++i)
-        if ((uint32_t)i == (id >> 5)) key[i] = 0;
+      for (int i = 0; i < EL; ++i) {
+        if ((uint32_t)i == gone) key[i] = 0;
+        if (key[i] > best) { best = key[i]; at = (uint32_t)i; }
+      }
     }
+  }
+  // the choices' logits from the lanes that hold them
+#pragma unroll
+  for (int i = 0; i < EL; ++i) {
+    const float v = __shfl_sync(kAll, x[i], my_id >= 0 ? my_id / EL : 0);
+    if (my_id >= 0 && my_id % EL == i) my_logit = v;
   }
   return __all_sync(kAll, sure);
 }
 
-// Rows of a block one after another by its warps.  Dynamic shared memory: counts [experts], then per warp the group scratch.
+// In 64 bits, from memory again (the rare case, out of the way of the other).
 template <int EL>
-__global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs a) {
-  pdl_prologue();
-  extern __shared__ unsigned char route_smem[];
-  uint32_t* hist = reinterpret_cast<uint32_t*>(route_smem);
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  double* scratch = reinterpret_cast<double*>(route_smem + ((a.experts * 4u + 15u) & ~15u)) + (size_t)warp * (a.experts + a.groups);
-  for (uint32_t e = threadIdx.x; e < a.experts; e += blockDim.x) hist[e] = 0u;
-  __syncthreads();
-  const uint32_t lo = blockIdx.x * a.block_rows, hi = min(lo + a.block_rows, a.tokens);
-  for (uint32_t t = lo + warp; t < hi; t += kRouteWarps) {
-    const bool on = !a.mask || a.mask[t] != 0u;
-    int id = -1;
-    float logit = 0.0f, w = 0.0f;
-    if (on) {
-      float x[EL];
-      float m = -INFINITY;
+__device__ __noinline__ int2 choose_exactly(const RouteArgs& a, float xmax, uint32_t t, uint32_t lane, double* strength) {
+  float x[EL], bias[EL], logit;
+  int id;
+  load_logits<EL>(a, t, lane, x);
 #pragma unroll
-      for (int i = 0; i < EL; ++i) {
-        const uint32_t e = lane + 32u * i;
-        float v = e < a.experts ? load_logit(a, t * a.logit_stride + e) : NAN;
-        if (v == INFINITY) v = 3.402823466e38f;
-        if (v == -INFINITY) v = NAN;
-        x[i] = v;
-        m = fmaxf(m, v);                  // (NaN counts as absent)
-      }
-      m = value_of(warp_max(key_of(m)));
-      if (!choose<float, EL>(a, x, m, lane, reinterpret_cast<float*>(scratch), id, logit))
-        choose<double, EL>(a, x, m, lane, scratch, id, logit);
-      const bool mine = id >= 0;
-      float s = 0.0f;
-      if (a.renormalise) {
-        // ratios of scores, without under- or overflow: softmax exp(x - top) and sigmoid
-        // exp(min(x, 0) - min(top, 0)) / (1 + exp(-|x|)) up to factors that the choices share
-        const float top = value_of(warp_max(mine ? key_of(logit) : 0u));
-        if (mine) s = a.sigmoid ? expf(fminf(logit, 0.0f) - fminf(top, 0.0f)) / (1.0f + expf(-fabsf(logit))) : expf(logit - top);
-        const float sum = warp_sum(s);
-        s = mine ? s / sum : 0.0f;
-      } else if (a.sigmoid) {
-        s = mine ? (logit >= 0.0f ? 1.0f / (1.0f + expf(-logit)) : expf(logit) / (1.0f + expf(logit))) : 0.0f;
-      } else {
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < EL; ++i) sum += x[i] == x[i] ? expf(x[i] - m) : 0.0f;
-        sum = warp_sum(sum);
-        s = mine ? expf(logit - m) / sum : 0.0f;
-      }
-      w = s * a.scaling;
-    }
-    if (lane < a.top_k) {
-      a.ids[(size_t)t * a.top_k + lane] = id;
-      a.weights[(size_t)t * a.top_k + lane] = id >= 0 ? w : 0.0f;
-      if (id >= 0) atomicAdd(&hist[id], 1u);
-    }
-  }
-  if (!a.counts) return;
-  __syncthreads();
-  for (uint32_t e = threadIdx.x; e < a.experts; e += blockDim.x) a.counts[(size_t)blockIdx.x * a.experts + e] = hist[e];
+  for (int i = 0; i < EL; ++i) bias[i] = a.bias && lane * EL + i < a.experts ? __ldcg(a.bias + lane * EL + i) : 0.0f;
+  choose<double, EL>(a, x, bias, xmax, t, lane, strength, id, logit);
+  return make_int2(id, __float_as_int(logit));
 }
 
-// Places the choices of each block.  Dynamic shared memory: places [experts] and, per expert, a bit for each row of
-// the block.
-__global__ void __launch_bounds__(512) order_kernel(const RouteArgs a) {
-  pdl_prologue();
-  extern __shared__ uint32_t order_smem[];
-  uint32_t *place = order_smem, *bits = order_smem + a.experts;
-  __shared__ uint32_t warp_total[16];
-  const uint32_t words = a.block_rows / 32u, lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  const uint32_t lo = blockIdx.x * a.block_rows, hi = min(lo + a.block_rows, a.tokens), choices = (hi - lo) * a.top_k;
-  for (uint32_t i = threadIdx.x; i < a.experts * words; i += blockDim.x) bits[i] = 0u;
-  // how many rows of all blocks, and of the blocks before this one, go to each expert; the first place of each expert
-  uint32_t carry = 0;
-  for (uint32_t e0 = 0; e0 < a.experts; e0 += blockDim.x) {
-    const uint32_t e = e0 + threadIdx.x;
-    uint32_t all = 0, before = 0;
-    if (e < a.experts) {
-#pragma unroll 8
-      for (uint32_t b = 0; b < a.blocks; ++b) {
-        const uint32_t c = __ldcg(a.counts + (size_t)b * a.experts + e);
-        all += c;
-        before += b < blockIdx.x ? c : 0u;
-      }
-    }
-    uint32_t up = all;
+// One row: its choices and their weights, by a warp.
+template <int EL>
+__device__ __forceinline__ void route_row(const RouteArgs& a, uint32_t t, const float (&x)[EL], const float (&bias)[EL], uint32_t lane,
+                                          double* scratch, int& id, float& w) {
+  float m = -INFINITY;
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const uint32_t o = __shfl_up_sync(kAll, up, d);
-      if (lane >= (uint32_t)d) up += o;
-    }
-    if (lane == 31u) warp_total[warp] = up;
-    __syncthreads();
-    uint32_t base = carry, total = 0;
-    for (uint32_t w = 0; w < blockDim.x / 32u; ++w) {
-      if (w < warp) base += warp_total[w];
-      total += warp_total[w];
-    }
-    if (e < a.experts) {
-      place[e] = base + up - all + before;
-      if (blockIdx.x == 0u) a.offsets[e] = (int32_t)(base + up - all);
-    }
-    carry += total;
-    __syncthreads();
+  for (int i = 0; i < EL; ++i) m = fmaxf(m, x[i]);      // (NaN counts as absent)
+  m = value_of(warp_max(key_of(m)));
+  float logit;
+  if (!choose<float, EL>(a, x, bias, m, t, lane, reinterpret_cast<float*>(scratch), id, logit)) {
+    const int2 exact = choose_exactly<EL>(a, m, t, lane, scratch);
+    id = exact.x;
+    logit = __int_as_float(exact.y);
   }
-  if (blockIdx.x == 0u && threadIdx.x == 0u) a.offsets[a.experts] = (int32_t)carry;
+  const bool mine = id >= 0;
+  float s = 0.0f;
+  if (a.renormalise) {
+    // ratios of scores, without under- or overflow: softmax exp(x - top) and sigmoid
+    // exp(min(x, 0) - min(top, 0)) / (1 + exp(-|x|)) up to factors that the choices share
+    const float top = value_of(warp_max(mine ? key_of(logit) : 0u));
+    if (mine) s = a.sigmoid ? expf(fminf(logit, 0.0f) - fminf(top, 0.0f)) / (1.0f + expf(-fabsf(logit))) : expf(logit - top);
+    const float sum = warp_sum(s);
+    s = mine ? s / sum : 0.0f;
+  } else if (a.sigmoid) {
+    s = mine ? (logit >= 0.0f ? 1.0f / (1.0f + expf(-logit)) : expf(logit) / (1.0f + expf(logit))) : 0.0f;
+  } else {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < EL; ++i) sum += x[i] == x[i] ? expf(x[i] - m) : 0.0f;
+    sum = warp_sum(sum);
+    s = mine ? expf(logit - m) / sum : 0.0f;
+  }
+  w = mine ? s * a.scaling : 0.0f;
+}
+
+// Places of the choices of rows [lo, hi).  Shared memory: place [experts], the first place of each expert for these rows, and
+// bits [experts][words], zeros, a bit for each of the rows.
+__device__ __forceinline__ void place_choices(const RouteArgs& a, uint32_t lo, uint32_t hi, const uint32_t* place, uint32_t* bits, uint32_t words) {
+  const uint32_t choices = (hi - lo) * a.top_k;
   for (uint32_t i = threadIdx.x; i < choices; i += blockDim.x) {
     const int id = __ldcg(a.ids + (size_t)lo * a.top_k + i);
     const uint32_t r = i / a.top_k;
@@ -325,6 +355,128 @@ __global__ void __launch_bounds__(512) order_kernel(const RouteArgs a) {
     }
     a.slot[(size_t)lo * a.top_k + i] = at;
   }
+}
+
+// Sums before each of up to blockDim.x numbers; all threads take part.  `total`: their sum.
+__device__ __forceinline__ uint32_t sum_before(uint32_t mine, uint32_t* warp_total, uint32_t& total) {
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  uint32_t up = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint32_t o = __shfl_up_sync(kAll, up, d);
+    if (lane >= (uint32_t)d) up += o;
+  }
+  if (lane == 31u) warp_total[warp] = up;
+  __syncthreads();
+  uint32_t base = 0;
+  total = 0;
+  for (uint32_t w = 0; w < blockDim.x / 32u; ++w) {
+    if (w < warp) base += warp_total[w];
+    total += warp_total[w];
+  }
+  __syncthreads();
+  return base + up - mine;
+}
+
+// Rows of a block one after another by its warps.  Dynamic shared memory: counts [experts]; where one block has all
+// rows, the bits of place_choices; then per warp the scratch of groups.
+template <int EL>
+__global__ void __launch_bounds__(kRouteThreads<EL>) route_kernel(const RouteArgs a) {
+  pdl_prologue();
+  extern __shared__ __align__(16) unsigned char route_smem[];
+  __shared__ uint32_t warp_total[32];
+  uint32_t* hist = reinterpret_cast<uint32_t*>(route_smem);
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, words = a.block_rows / 32u;
+  const uint32_t ints = a.experts * (a.alone ? 1u + words : 1u);
+  double* scratch = reinterpret_cast<double*>(route_smem + ((ints * 4u + 15u) & ~15u)) + (size_t)warp * (a.experts + a.groups);
+  for (uint32_t e = threadIdx.x; e < ints; e += blockDim.x) hist[e] = 0u;
+  float bias[EL];
+#pragma unroll
+  for (int i = 0; i < EL; ++i) bias[i] = a.bias && lane * EL + i < a.experts ? __ldcg(a.bias + lane * EL + i) : 0.0f;
+  __syncthreads();
+  const uint32_t lo = blockIdx.x * a.block_rows, hi = min(lo + a.block_rows, a.tokens), step = blockDim.x >> 5;
+  float x[EL];
+  if (lo + warp < hi) load_logits<EL>(a, lo + warp, lane, x);
+  for (uint32_t t = lo + warp; t < hi; t += step) {
+    const bool on = !a.mask || a.mask[t] != 0u;
+    int id = -1;
+    float w = 0.0f;
+    if (on) route_row<EL>(a, t, x, bias, lane, scratch, id, w);
+    if (t + step < hi) load_logits<EL>(a, t + step, lane, x);
+    if (lane < a.top_k) {
+      a.ids[(size_t)t * a.top_k + lane] = id;
+      a.weights[(size_t)t * a.top_k + lane] = w;
+      if (id >= 0) atomicAdd(&hist[id], 1u);
+    }
+  }
+  if (!a.order) return;
+  __syncthreads();
+  if (!a.alone) {
+    for (uint32_t e = threadIdx.x; e < a.experts; e += blockDim.x) a.counts[(size_t)blockIdx.x * a.experts + e] = hist[e];
+    return;
+  }
+  uint32_t carry = 0;
+  for (uint32_t e0 = 0; e0 < a.experts; e0 += blockDim.x) {
+    const uint32_t e = e0 + threadIdx.x;
+    uint32_t total;
+    const uint32_t before = carry + sum_before(e < a.experts ? hist[e] : 0u, warp_total, total);
+    if (e < a.experts) {
+      hist[e] = before;
+      a.offsets[e] = (int32_t)before;
+    }
+    carry += total;
+  }
+  if (threadIdx.x == 0u) a.offsets[a.experts] = (int32_t)carry;
+  __syncthreads();
+  place_choices(a, lo, hi, hist, hist + a.experts, words);
+  for (uint32_t i = carry + threadIdx.x; i < a.tokens * a.top_k; i += blockDim.x) a.order[i] = -1;
+}
+
+// Places the choices of each block.  Dynamic shared memory: places [experts], the bits of place_choices, partial sums [1024][2].
+__global__ void __launch_bounds__(1024) order_kernel(const RouteArgs a) {
+  pdl_prologue();
+  extern __shared__ uint32_t order_smem[];
+  __shared__ uint32_t warp_total[32];
+  const uint32_t words = a.block_rows / 32u;
+  uint32_t *place = order_smem, *bits = place + a.experts, *sums = bits + a.experts * words;
+  const uint32_t lo = blockIdx.x * a.block_rows, hi = min(lo + a.block_rows, a.tokens);
+  for (uint32_t i = threadIdx.x; i < a.experts * words; i += blockDim.x) bits[i] = 0u;
+  // how many rows of all blocks, and of the blocks before this one, go to each expert: a.share threads add up an expert's counts
+  uint32_t carry = 0;
+  const uint32_t at_once = blockDim.x / a.share, part = threadIdx.x / at_once;
+  const uint32_t b_lo = a.blocks * part / a.share, b_hi = a.blocks * (part + 1u) / a.share;
+  for (uint32_t e0 = 0; e0 < a.experts; e0 += at_once) {
+    const uint32_t e = e0 + threadIdx.x % at_once;
+    uint32_t all = 0, before = 0;
+    if (e < a.experts) {
+#pragma unroll 8
+      for (uint32_t b = b_lo; b < b_hi; ++b) {
+        const uint32_t c = __ldcg(a.counts + (size_t)b * a.experts + e);
+        all += c;
+        before += b < blockIdx.x ? c : 0u;
+      }
+    }
+    sums[threadIdx.x] = all;
+    sums[blockDim.x + threadIdx.x] = before;
+    __syncthreads();
+    all = before = 0;
+    if (part == 0u && e < a.experts) {
+      for (uint32_t q = 0; q < a.share; ++q) {
+        all += sums[q * at_once + threadIdx.x];
+        before += sums[blockDim.x + q * at_once + threadIdx.x];
+      }
+    }
+    uint32_t total;
+    const uint32_t start = carry + sum_before(all, warp_total, total);
+    if (part == 0u && e < a.experts) {
+      place[e] = start + before;
+      if (blockIdx.x == 0u) a.offsets[e] = (int32_t)start;
+    }
+    carry += total;
+  }
+  if (blockIdx.x == 0u && threadIdx.x == 0u) a.offsets[a.experts] = (int32_t)carry;
+  __syncthreads();
+  place_choices(a, lo, hi, place, bits, words);
   // behind the last
   const uint64_t end = (uint64_t)a.tokens * a.top_k;
   for (uint64_t i = carry + (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < end; i += (uint64_t)gridDim.x * blockDim.x) a.order[i] = -1;
@@ -457,26 +609,34 @@ cudaError_t launch_route(const void* logits, const float* bias, const uint8_t* m
   a.offsets = offsets;
   a.order = order;
   a.slot = slot;
-  a.counts = order ? (uint32_t*)counts : nullptr;
+  a.counts = (uint32_t*)counts;
   a.block_rows = rows_of_a_block(d);
   a.blocks = (d.tokens + a.block_rows - 1u) / a.block_rows;
-  const size_t smem = ((d.experts * 4u + 15u) & ~15u) + (d.groups > 1u ? sizeof(double) * kRouteWarps * (d.experts + d.groups) : 0u);
-  const uint32_t per_lane = (d.experts + 31u) / 32u;
-  auto go = [&](auto kernel) {
+  a.alone = a.blocks == 1u;
+  a.wide = (((uintptr_t)logits | d.logit_stride * (d.in_dtype == PSB_DT_F32 ? 4u : 2u)) & 15u) == 0u;
+  uint32_t el = 1;
+  while (el * 32u < d.experts) el *= 2u;
+  const uint32_t size = d.experts / d.groups, lanes = size / el;
+  a.lanes_per_group = size % el == 0u && (lanes & (lanes - 1u)) == 0u ? lanes : 0u;
+  a.share = 1;
+  while (a.share < 32u && a.share * 2u * d.experts <= 1024u) a.share *= 2u;
+  const uint32_t ints = d.experts * (a.alone ? 1u + a.block_rows / 32u : 1u);
+  auto go = [&](auto kernel, uint32_t threads) {
+    const size_t smem = ((ints * 4u + 15u) & ~15u) + (d.groups > 1u ? sizeof(double) * (threads / 32u) * (d.experts + d.groups) : 0u);
     if (smem > 48u * 1024u) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    launch_pdl(kernel, a.blocks, kRouteWarps * 32u, smem, s, a);
+    launch_pdl(kernel, a.blocks, threads, smem, s, a);
   };
-  if (per_lane <= 1u) go(route_kernel<1>);
-  else if (per_lane <= 2u) go(route_kernel<2>);
-  else if (per_lane <= 4u) go(route_kernel<4>);
-  else if (per_lane <= 8u) go(route_kernel<8>);
-  else if (per_lane <= 16u) go(route_kernel<16>);
-  else go(route_kernel<32>);
+  if (el == 1u) go(route_kernel<1>, kRouteThreads<1>);
+  else if (el == 2u) go(route_kernel<2>, kRouteThreads<2>);
+  else if (el == 4u) go(route_kernel<4>, kRouteThreads<4>);
+  else if (el == 8u) go(route_kernel<8>, kRouteThreads<8>);
+  else if (el == 16u) go(route_kernel<16>, kRouteThreads<16>);
+  else go(route_kernel<32>, kRouteThreads<32>);
   note_launch();
-  if (order) {
-    const size_t bytes = sizeof(uint32_t) * d.experts * (1u + a.block_rows / 32u);
+  if (order && !a.alone) {
+    const size_t bytes = sizeof(uint32_t) * (d.experts * (1u + a.block_rows / 32u) + 2048u);
     if (bytes > 48u * 1024u) cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    launch_pdl(order_kernel, a.blocks, 512, bytes, s, a);
+    launch_pdl(order_kernel, a.blocks, 1024, bytes, s, a);
     note_launch();
   }
   return cudaGetLastError();
