@@ -3,7 +3,7 @@
 // route: a row's experts are those of the top_k largest select values.  Near the border two values may differ by less
 // than fp32 resolves, and a row sent to another expert is a wrong answer, so the comparison is exact: without a bias the
 // scores are monotone in the logits and the logits themselves are compared; otherwise fp32 values decide wherever
-// they are further apart than their error bound (kDoubt), and the row is done again in 64 bits where they are not (equal
+// they are further apart than their error bound (kRound), and the row is done again in 64 bits where they are not (equal
 // logits with equal biases are equal, and need no second look).
 // The order of the choices is a counting sort: blocks of consecutive rows count their choices per expert; the
 // second launch adds up the counts of the blocks before it and places its own, the rank inside a block being the number of
@@ -18,11 +18,14 @@ namespace psb {
 namespace {
 
 constexpr uint32_t kAll = 0xFFFFFFFFu;
-template <int EL> constexpr uint32_t kRouteThreads = EL <= 8 ? 512u : 256u;
+template <int EL> constexpr uint32_t kRouteThreads = EL <= 8 ? 1024u : 256u;
 constexpr uint32_t kMaxBlockRows = 1024;   // rows of a counting block: 32 words of a bit mask
-// Error of fp32 select values, relative to 1 + |value|: scores are at most 1 and their errors below 2e-6 (32 added terms a lane and five
-// of the tree, exp, quotient), the bias rounds once.  Two values are compared, hence twice.
-constexpr float kDoubt = 8e-6f;
+// Two fp32 select values are told apart if they differ by more than unit + kRound * (|v| + |w|).  exp is off by 2^-22 and 2^-24 of its argument,
+// relatively, a quotient by 2^-23.  A sigmoid p changes by p (1 - p) of exp's error: 1/4 of 2^-22, 0.23 of 2^-24, and its sum and quotient
+// round: below 3e-7 in all.  A softmax has the errors of exp twice, the quotient's and those of the sum of `el` numbers a lane and five
+// levels of lanes, all of them of the row's largest score at most.  Two values, hence twice.  The bias rounds once, 2^-24 of the value.
+constexpr float kSigmoidUnit = 6e-7f, kRound = 1.2e-7f;
+__host__ __device__ constexpr float softmax_unit(int el) { return 2.0f * (8e-7f + 6e-8f * (float)(el + 5)); }
 
 struct RouteArgs {
   const void* logits;
@@ -33,22 +36,20 @@ struct RouteArgs {
   uint64_t logit_stride;
   int32_t *ids, *offsets, *order, *slot;
   float* weights;
-  uint32_t* counts;        // [blocks][experts]
+  uint32_t* counts;        // [blocks + 1][experts]
   uint32_t block_rows, blocks;
   uint32_t alone;            // one block has all rows and places them itself
   uint32_t wide;             // rows of logits start at multiples of 16 bytes
   uint32_t lanes_per_group;  // a power of two where groups are the experts of whole lanes, else 0
-  uint32_t share;            // threads that add up the counts of an expert
 };
 
-// Monotone map of fp32 numbers onto words, 0 below all of them.
-__device__ __forceinline__ uint32_t key_of(float v) {
-  const uint32_t u = __float_as_uint(v);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+// Monotone map of fp32 numbers onto words, kNone below all of them; and of fp64 numbers, 0 below all of them.
+constexpr int kNone = (int)0x80000000;
+__device__ __forceinline__ int key_of(float v) {
+  const int u = __float_as_int(v);
+  return u ^ ((u >> 31) & 0x7FFFFFFF);
 }
-__device__ __forceinline__ float value_of(uint32_t key) {
-  return __uint_as_float((key & 0x80000000u) ? (key & 0x7FFFFFFFu) : ~key);
-}
+__device__ __forceinline__ float value_of(int key) { return __int_as_float(key ^ ((key >> 31) & 0x7FFFFFFF)); }
 __device__ __forceinline__ unsigned long long key_of(double v) {
   const unsigned long long u = (unsigned long long)__double_as_longlong(v);
   return (u >> 63) ? ~u : (u | (1ull << 63));
@@ -56,7 +57,7 @@ __device__ __forceinline__ unsigned long long key_of(double v) {
 __device__ __forceinline__ double value_of(unsigned long long key) {
   return __longlong_as_double((long long)((key >> 63) ? (key & ~(1ull << 63)) : ~key));
 }
-__device__ __forceinline__ uint32_t warp_max(uint32_t v) { return __reduce_max_sync(kAll, v); }
+__device__ __forceinline__ int warp_max(int v) { return __reduce_max_sync(kAll, v); }
 __device__ __forceinline__ unsigned long long warp_max(unsigned long long v) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) {
@@ -77,16 +78,9 @@ __device__ __forceinline__ float load_logit(const RouteArgs& a, uint64_t at) {
   return __half2float(((const __half*)a.logits)[at]);
 }
 
-__device__ __forceinline__ float quotient(float p, float q) { return __fdividef(p, q); }      // 2 ulp
-__device__ __forceinline__ double quotient(double p, double q) { return p / q; }
-
-template <typename F> struct KeyType;
-template <> struct KeyType<float> { typedef uint32_t type; };
-template <> struct KeyType<double> { typedef unsigned long long type; };
-
-template <typename F> __device__ __forceinline__ F exp_of(F x);
-template <> __device__ __forceinline__ float exp_of<float>(float x) { return __expf(x); }
-template <> __device__ __forceinline__ double exp_of<double>(double x) { return exp(x); }
+// A logit as it counts: NaN where the expert is not available.
+__device__ __forceinline__ float clean(float v) { return v == INFINITY ? 3.402823466e38f : v == -INFINITY ? NAN : v; }
+__device__ __forceinline__ float load_clean(const RouteArgs& a, uint64_t at) { return clean(load_logit(a, at)); }
 
 // The lane's logits, experts lane * EL ...; NaN where there is no such expert or it is not available.
 template <int EL>
@@ -117,16 +111,13 @@ __device__ __forceinline__ void load_logits(const RouteArgs& a, uint32_t t, uint
     for (int i = 0; i < EL; ++i) x[i] = e0 + i < a.experts ? load_logit(a, at + i) : NAN;
   }
 #pragma unroll
-  for (int i = 0; i < EL; ++i) {
-    if (x[i] == INFINITY) x[i] = 3.402823466e38f;
-    if (x[i] == -INFINITY) x[i] = NAN;
-  }
+  for (int i = 0; i < EL; ++i) x[i] = clean(x[i]);
 }
 
 // Whether two experts of a row have the same logit and the same bias (a look at memory: the registers are another lane's).
 __device__ __noinline__ bool same_select(const RouteArgs& a, uint32_t t, uint32_t e, uint32_t o) {
   return load_logit(a, (uint64_t)t * a.logit_stride + e) == load_logit(a, (uint64_t)t * a.logit_stride + o) &&
-         (!a.bias || __ldcg(a.bias + e) == __ldcg(a.bias + o));
+         (!a.bias || __ldca(a.bias + e) == __ldca(a.bias + o));
 }
 
 // The two largest keys of a run of experts, put together with those of another run.
@@ -138,95 +129,97 @@ __device__ __forceinline__ void merge_best(Key& first, Key& second, Key f, Key s
   second = low > second ? low : second;
 }
 
-// The choices of one row, by a warp; lane l holds experts l * EL ...  Lane j < top_k receives choice j (id -1: none)
-// and its logit.  Returns whether the comparisons were certain (F = double: always).
-template <typename F, int EL>
+// The choices of one row, by a warp; lane l holds experts l * EL ...  Lane j < top_k receives choice j (id -1: none).
+// Returns whether the comparisons were certain (if not: choose_exactly).
+template <int EL>
 __device__ __forceinline__ bool choose(const RouteArgs& a, const float (&x)[EL], const float (&bias)[EL], float xmax, uint32_t t,
-                                       uint32_t lane, F* strength, int& my_id, float& my_logit) {
-  typedef typename KeyType<F>::type Key;
-  const bool exact_type = sizeof(F) == 8;
+                                       uint32_t lane, int* scratch, int& my_id) {
   const bool by_logit = !a.bias && a.groups == 1u;      // scores are monotone in the logits
-  Key key[EL];
+  int key[EL];
   bool sure = true;
+  float unit = kSigmoidUnit;
   if (by_logit) {
 #pragma unroll
-    for (int i = 0; i < EL; ++i) key[i] = x[i] == x[i] ? key_of((F)(x[i] + 0.0f)) : (Key)0;     // (-0 and 0 are equal)
+    for (int i = 0; i < EL; ++i) key[i] = x[i] == x[i] ? key_of(x[i] + 0.0f) : kNone;     // (-0 and 0 are equal)
   } else {
-    F p[EL];
+    float p[EL];
     if (a.sigmoid) {
 #pragma unroll
-      for (int i = 0; i < EL; ++i) p[i] = quotient((F)1, (F)1 + exp_of<F>(-(F)x[i]));
+      for (int i = 0; i < EL; ++i) p[i] = __fdividef(1.0f, 1.0f + __expf(-x[i]));
     } else {
-      F sum = 0;
+      float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < EL; ++i) {
-        p[i] = exp_of<F>((F)x[i] - (F)xmax);
-        sum += x[i] == x[i] ? p[i] : (F)0;
+        p[i] = __expf(x[i] - xmax);
+        sum += x[i] == x[i] ? p[i] : 0.0f;
       }
       sum = warp_sum(sum);
+      unit = softmax_unit(EL) / sum;      // (the largest score is 1 / sum)
 #pragma unroll
-      for (int i = 0; i < EL; ++i) p[i] = quotient(p[i], sum);
+      for (int i = 0; i < EL; ++i) p[i] = __fdividef(p[i], sum);
     }
 #pragma unroll
     for (int i = 0; i < EL; ++i) {
-      const F sel = p[i] + (F)bias[i];
-      key[i] = x[i] == x[i] && sel == sel ? key_of(sel + (F)0) : (Key)0;
+      const float sel = p[i] + bias[i];         // (NaN where x is)
+      key[i] = sel == sel ? key_of(sel + 0.0f) : kNone;
     }
     if (a.groups > 1u) {
       const uint32_t size = a.experts / a.groups;
       uint32_t stay = 0;       // bit i: my expert i stays
       if (a.lanes_per_group) {
         // a group is the experts of 1, 2, 4 ... lanes: every lane learns its group's strength
-        Key first = 0, second = 0;
+        int first = kNone, second = kNone;
 #pragma unroll
-        for (int i = 0; i < EL; ++i) merge_best(first, second, key[i], (Key)0);
+        for (int i = 0; i < EL; ++i) merge_best(first, second, key[i], kNone);
         for (uint32_t d = 1; d < a.lanes_per_group; d <<= 1) {
-          const Key f = __shfl_xor_sync(kAll, first, (int)d), s = __shfl_xor_sync(kAll, second, (int)d);
+          const int f = __shfl_xor_sync(kAll, first, (int)d), s = __shfl_xor_sync(kAll, second, (int)d);
           merge_best(first, second, f, s);
         }
-        const bool two = second && a.group_best > 1u;
-        const Key mine = !first ? (Key)0 : key_of((two ? value_of(first) + value_of(second) : value_of(first)) + (F)0);
-        const float far = exact_type ? 0.0f : kDoubt * (2.0f + fabsf((float)value_of(first)) + (two ? fabsf((float)value_of(second)) : 0.0f));
+        const bool two = second != kNone && a.group_best > 1u;
+        const float v1 = value_of(first), v2 = two ? value_of(second) : 0.0f;
+        const uint32_t head = lane & ~(a.lanes_per_group - 1u);
+        const bool real = lane < a.groups * a.lanes_per_group;
+        const int mine = first == kNone || !real ? kNone : key_of(v1 + v2);
         uint32_t before = 0;
-        for (uint32_t g = 0; g < a.groups; ++g) {
-          const uint32_t from = g * a.lanes_per_group;
-          const Key k = __shfl_sync(kAll, mine, (int)from);
-          before += (k > mine || (k == mine && from < (lane & ~(a.lanes_per_group - 1u)))) ? 1u : 0u;
-          if (!exact_type) {
-            const float doubt = far + __shfl_sync(kAll, far, (int)from);
-            if (mine && k && from != (lane & ~(a.lanes_per_group - 1u)))
-              sure = sure && fabsf((float)value_of(k) - (float)value_of(mine)) > doubt;
-          }
+        for (uint32_t from = 0; from < a.groups * a.lanes_per_group; from += a.lanes_per_group) {
+          const int k = __shfl_sync(kAll, mine, (int)from);
+          before += (k > mine || (k == mine && from < head)) ? 1u : 0u;
         }
         stay = before < a.top_groups ? 0xFFFFFFFFu : 0u;
-        sure = sure || lane >= a.groups * a.lanes_per_group;
+        if (a.top_groups < a.groups) {
+          // the weakest group that stays against the strongest that does not
+          const int in = ~warp_max(real && stay ? ~mine : kNone), out = warp_max(real && !stay ? mine : kNone);
+          const float far = value_of(warp_max(mine != kNone ? key_of(fabsf(v1) + fabsf(v2)) : 0));
+          if (in != kNone && out != kNone) sure = value_of(in) - value_of(out) > 2.0f * unit + 4.0f * kRound * far;
+        }
       } else {
         // strengths through shared memory: lane g takes groups g, g + 32, ...
-        Key* all = reinterpret_cast<Key*>(strength);           // [experts]
+        int* all = scratch;                                    // [experts]
 #pragma unroll
         for (int i = 0; i < EL; ++i)
           if (lane * EL + i < a.experts) all[lane * EL + i] = key[i];
         __syncwarp();
-        Key* group = all + a.experts;                          // [groups]
-        F* size_of = reinterpret_cast<F*>(group + a.groups);   // [groups] magnitudes behind the strengths (fp32 alone)
+        int* group = all + a.experts;                          // [groups]
+        float* size_of = reinterpret_cast<float*>(group + a.groups);   // [groups] magnitudes behind the strengths
         for (uint32_t g = lane; g < a.groups; g += 32u) {
-          Key first = 0, second = 0;
-          for (uint32_t j = 0; j < size; ++j) merge_best(first, second, all[g * size + j], (Key)0);
-          const bool two = second && a.group_best > 1u;
-          group[g] = !first ? (Key)0 : key_of((two ? value_of(first) + value_of(second) : value_of(first)) + (F)0);
-          if (!exact_type) size_of[g] = (F)2 + (F)fabsf((float)value_of(first)) + (two ? (F)fabsf((float)value_of(second)) : (F)0);
+          int first = kNone, second = kNone;
+          for (uint32_t j = 0; j < size; ++j) merge_best(first, second, all[g * size + j], kNone);
+          const bool two = second != kNone && a.group_best > 1u;
+          const float v1 = value_of(first), v2 = two ? value_of(second) : 0.0f;
+          group[g] = first == kNone ? kNone : key_of(v1 + v2 + 0.0f);
+          size_of[g] = fabsf(v1) + fabsf(v2);
         }
         __syncwarp();
         // a group stays if fewer than top_groups are stronger, or as strong and before it
         for (uint32_t g0 = 0; g0 < a.groups; g0 += 32u) {
           const uint32_t g = g0 + lane;
-          const Key mine = g < a.groups ? group[g] : (Key)0;
+          const int mine = g < a.groups ? group[g] : kNone;
           uint32_t before = 0;
           for (uint32_t o = 0; o < a.groups; ++o) {
-            const Key k = group[o];
+            const int k = group[o];
             before += (k > mine || (k == mine && o < g)) ? 1u : 0u;
-            if (!exact_type && g < a.groups && o != g && mine && k)
-              sure = sure && fabsf((float)value_of(k) - (float)value_of(mine)) > kDoubt * ((float)size_of[g] + (float)size_of[o]);
+            if (o != g && mine != kNone && k != kNone)
+              sure = sure && fabsf(value_of(k) - value_of(mine)) > 2.0f * unit + 2.0f * kRound * (size_of[g] + size_of[o]);
           }
           const uint32_t in = __ballot_sync(kAll, g < a.groups && before < a.top_groups);
 #pragma unroll
@@ -239,63 +232,113 @@ __device__ __forceinline__ bool choose(const RouteArgs& a, const float (&x)[EL],
       }
 #pragma unroll
       for (int i = 0; i < EL; ++i)
-        if (!((stay >> i) & 1u)) key[i] = 0;
+        if (!((stay >> i) & 1u)) key[i] = kNone;
     }
   }
-  my_id = -1;
-  my_logit = 0.0f;
-  // the lane's best, found again only where it has been taken
-  Key best = 0;
-  uint32_t at = 0;
+  // the lane's two best; the third is looked for only where both have been taken
+  int best = kNone, next = kNone;
+  uint32_t at = 0, next_at = 0;
 #pragma unroll
-  for (int i = 0; i < EL; ++i)
-    if (key[i] > best) { best = key[i]; at = (uint32_t)i; }
-  Key last = 0;
-  uint32_t last_id = 0;
+  for (int i = 0; i < EL; ++i) {
+    if (key[i] > best) { next = best; next_at = at; best = key[i]; at = (uint32_t)i; }
+    else if (key[i] > next) { next = key[i]; next_at = (uint32_t)i; }
+  }
+  uint32_t taken = 0;          // bit i: my expert i
+  my_id = -1;
+  int my_key = kNone;
   // one round more than there are choices: is the last choice certain against the first that is left out
-  const uint32_t rounds = a.top_k + (exact_type || by_logit ? 0u : 1u);
+  const uint32_t rounds = a.top_k + (by_logit || a.top_k == 32u ? 0u : 1u);
   for (uint32_t j = 0; j < rounds; ++j) {
-    const Key top = warp_max(best);
-    if (!top) break;
+    const int top = warp_max(best);
+    if (top == kNone) break;
     const uint32_t from = (uint32_t)__ffs((int)__ballot_sync(kAll, best == top)) - 1u;     // the lowest lane, the lowest expert
     const uint32_t id = from * EL + __shfl_sync(kAll, at, (int)from);
-    if (!exact_type && !by_logit && j > 0u) {
-      const float v = (float)value_of(top), gap = (float)value_of(last) - v;
-      // (equal logits under equal biases are equal)
-      if (!(gap > kDoubt * (1.0f + fabsf(v)))) sure = sure && same_select(a, t, id, last_id);
-    }
-    last = top;
-    last_id = id;
-    if (j < a.top_k && lane == j) my_id = (int)id;
+    if (lane == j) { my_id = (int)id; my_key = top; }
     if (lane == from) {
-      best = 0;
-      const uint32_t gone = at;
+      taken |= 1u << at;
+      best = next;
+      at = next_at;
+      next = kNone;
+      if (best == kNone && EL > 2) {
 #pragma unroll
-      for (int i = 0; i < EL; ++i) {
-        if ((uint32_t)i == gone) key[i] = 0;
-        if (key[i] > best) { best = key[i]; at = (uint32_t)i; }
+        for (int i = 0; i < EL; ++i)
+          if (!((taken >> i) & 1u) && key[i] > best) { best = key[i]; at = (uint32_t)i; }
       }
     }
   }
-  // the choices' logits from the lanes that hold them
-#pragma unroll
-  for (int i = 0; i < EL; ++i) {
-    const float v = __shfl_sync(kAll, x[i], my_id >= 0 ? my_id / EL : 0);
-    if (my_id >= 0 && my_id % EL == i) my_logit = v;
+  if (!by_logit) {
+    // each choice against the next (equal logits under equal biases are equal)
+    const int other = __shfl_down_sync(kAll, my_key, 1), other_id = __shfl_down_sync(kAll, my_id, 1);
+    const float v = value_of(my_key), w = value_of(other);
+    if (lane < a.top_k && lane < 31u && my_id >= 0 && other_id >= 0 && !(v - w > unit + kRound * (fabsf(v) + fabsf(w))))
+      sure = sure && same_select(a, t, (uint32_t)my_id, (uint32_t)other_id);
+    if (a.top_k == 32u) sure = false;           // (no lane for the first that is left out)
   }
+  if (lane >= a.top_k) my_id = -1;
   return __all_sync(kAll, sure);
 }
 
-// In 64 bits, from memory again (the rare case, out of the way of the other).
-template <int EL>
-__device__ __noinline__ int2 choose_exactly(const RouteArgs& a, float xmax, uint32_t t, uint32_t lane, double* strength) {
-  float x[EL], bias[EL], logit;
-  int id;
-  load_logits<EL>(a, t, lane, x);
-#pragma unroll
-  for (int i = 0; i < EL; ++i) bias[i] = a.bias && lane * EL + i < a.experts ? __ldcg(a.bias + lane * EL + i) : 0.0f;
-  choose<double, EL>(a, x, bias, xmax, t, lane, strength, id, logit);
-  return make_int2(id, __float_as_int(logit));
+// The choices of one row in 64 bits, from memory again.  The rare case: its code is met cold, line by line, by the one warp
+// that needs it, while the other warps of the launch finish, so it is short (loops through shared memory, no unrolled copies
+// of exp: 30 us of a launch otherwise).  `keys`: [experts + groups].
+__device__ __noinline__ int choose_exactly(const RouteArgs& a, float xmax, uint32_t t, uint32_t lane, unsigned long long* keys) {
+  typedef unsigned long long Key;
+  const uint64_t row = (uint64_t)t * a.logit_stride;
+  double sum = 0.0;
+#pragma unroll 1
+  for (uint32_t pass = a.sigmoid ? 1u : 0u; pass < 2u; ++pass) {
+#pragma unroll 1
+    for (uint32_t e = lane; e < a.experts; e += 32u) {
+      const double x = (double)load_clean(a, row + e), v = exp(a.sigmoid ? -x : x - (double)xmax);
+      if (pass == 0u) {
+        if (x == x) sum += v;
+      } else {
+        const double sel = (a.sigmoid ? 1.0 : v) / (a.sigmoid ? 1.0 + v : sum) + (a.bias ? (double)__ldca(a.bias + e) : 0.0);
+        keys[e] = x == x && sel == sel ? key_of(sel + 0.0) : (Key)0;
+      }
+    }
+    if (pass == 0u) sum = warp_sum(sum);
+  }
+  __syncwarp();
+  const uint32_t size = a.experts / a.groups;
+  if (a.groups > 1u) {
+    Key* group = keys + a.experts;
+#pragma unroll 1
+    for (uint32_t g = lane; g < a.groups; g += 32u) {
+      Key first = 0, second = 0;
+#pragma unroll 1
+      for (uint32_t j = 0; j < size; ++j) merge_best(first, second, keys[g * size + j], (Key)0);
+      group[g] = !first ? (Key)0 : key_of((second && a.group_best > 1u ? value_of(first) + value_of(second) : value_of(first)) + 0.0);
+    }
+    __syncwarp();
+#pragma unroll 1
+    for (uint32_t g = lane; g < a.groups; g += 32u) {
+      uint32_t before = 0;
+#pragma unroll 1
+      for (uint32_t o = 0; o < a.groups; ++o) before += (group[o] > group[g] || (group[o] == group[g] && o < g)) ? 1u : 0u;
+      if (before >= a.top_groups) {
+#pragma unroll 1
+        for (uint32_t j = 0; j < size; ++j) keys[g * size + j] = 0;
+      }
+    }
+    __syncwarp();
+  }
+  int id = -1;
+#pragma unroll 1
+  for (uint32_t j = 0; j < a.top_k; ++j) {
+    Key best = 0;
+    uint32_t at = 0xFFFFFFFFu;
+#pragma unroll 1
+    for (uint32_t e = lane; e < a.experts; e += 32u)
+      if (keys[e] > best) { best = keys[e]; at = e; }
+    const Key top = warp_max(best);
+    if (!top) break;
+    const uint32_t e = __reduce_min_sync(kAll, best == top ? at : 0xFFFFFFFFu);
+    if (lane == j) id = (int)e;
+    if (e % 32u == lane) keys[e] = 0;
+    __syncwarp();
+  }
+  return id;
 }
 
 // One row: its choices and their weights, by a warp.
@@ -306,18 +349,15 @@ __device__ __forceinline__ void route_row(const RouteArgs& a, uint32_t t, const 
 #pragma unroll
   for (int i = 0; i < EL; ++i) m = fmaxf(m, x[i]);      // (NaN counts as absent)
   m = value_of(warp_max(key_of(m)));
-  float logit;
-  if (!choose<float, EL>(a, x, bias, m, t, lane, reinterpret_cast<float*>(scratch), id, logit)) {
-    const int2 exact = choose_exactly<EL>(a, m, t, lane, scratch);
-    id = exact.x;
-    logit = __int_as_float(exact.y);
-  }
+  if (!choose<EL>(a, x, bias, m, t, lane, reinterpret_cast<int*>(scratch), id))
+    id = choose_exactly(a, m, t, lane, reinterpret_cast<unsigned long long*>(scratch));
   const bool mine = id >= 0;
+  const float logit = mine ? load_clean(a, (uint64_t)t * a.logit_stride + (uint32_t)id) : 0.0f;
   float s = 0.0f;
   if (a.renormalise) {
     // ratios of scores, without under- or overflow: softmax exp(x - top) and sigmoid
     // exp(min(x, 0) - min(top, 0)) / (1 + exp(-|x|)) up to factors that the choices share
-    const float top = value_of(warp_max(mine ? key_of(logit) : 0u));
+    const float top = value_of(warp_max(mine ? key_of(logit) : kNone));
     if (mine) s = a.sigmoid ? expf(fminf(logit, 0.0f) - fminf(top, 0.0f)) / (1.0f + expf(-fabsf(logit))) : expf(logit - top);
     const float sum = warp_sum(s);
     s = mine ? s / sum : 0.0f;
@@ -386,13 +426,14 @@ __global__ void __launch_bounds__(kRouteThreads<EL>) route_kernel(const RouteArg
   extern __shared__ __align__(16) unsigned char route_smem[];
   __shared__ uint32_t warp_total[32];
   uint32_t* hist = reinterpret_cast<uint32_t*>(route_smem);
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, words = a.block_rows / 32u;
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, words = (a.block_rows + 31u) / 32u;
   const uint32_t ints = a.experts * (a.alone ? 1u + words : 1u);
   double* scratch = reinterpret_cast<double*>(route_smem + ((ints * 4u + 15u) & ~15u)) + (size_t)warp * (a.experts + a.groups);
   for (uint32_t e = threadIdx.x; e < ints; e += blockDim.x) hist[e] = 0u;
   float bias[EL];
 #pragma unroll
-  for (int i = 0; i < EL; ++i) bias[i] = a.bias && lane * EL + i < a.experts ? __ldcg(a.bias + lane * EL + i) : 0.0f;
+  // (through L1: every warp of the machine asking L2 for the same few lines took 20 us)
+  for (int i = 0; i < EL; ++i) bias[i] = a.bias && lane * EL + i < a.experts ? __ldca(a.bias + lane * EL + i) : 0.0f;
   __syncthreads();
   const uint32_t lo = blockIdx.x * a.block_rows, hi = min(lo + a.block_rows, a.tokens), step = blockDim.x >> 5;
   float x[EL];
@@ -400,9 +441,11 @@ __global__ void __launch_bounds__(kRouteThreads<EL>) route_kernel(const RouteArg
   for (uint32_t t = lo + warp; t < hi; t += step) {
     const bool on = !a.mask || a.mask[t] != 0u;
     int id = -1;
-    float w = 0.0f;
+    float w = 0.0f, next[EL];
+    if (t + step < hi) load_logits<EL>(a, t + step, lane, next);
     if (on) route_row<EL>(a, t, x, bias, lane, scratch, id, w);
-    if (t + step < hi) load_logits<EL>(a, t + step, lane, x);
+#pragma unroll
+    for (int i = 0; i < EL; ++i) x[i] = next[i];
     if (lane < a.top_k) {
       a.ids[(size_t)t * a.top_k + lane] = id;
       a.weights[(size_t)t * a.top_k + lane] = w;
@@ -432,60 +475,63 @@ __global__ void __launch_bounds__(kRouteThreads<EL>) route_kernel(const RouteArg
   for (uint32_t i = carry + threadIdx.x; i < a.tokens * a.top_k; i += blockDim.x) a.order[i] = -1;
 }
 
-// Places the choices of each block.  Dynamic shared memory: places [experts], the bits of place_choices, partial sums [1024][2].
+// Turns the counts of the blocks into the numbers of rows before each block, expert by expert, and adds the sums as one row more.
+// 32 experts a block of threads, the counting blocks dealt out to 32 threads each.  (Every placing block adding up all
+// counts took 12 us of 148 SMs on the same 150 KB.)
+__global__ void __launch_bounds__(1024) scan_kernel(const RouteArgs a) {
+  pdl_prologue();
+  __shared__ uint32_t sums[32][33];
+  const uint32_t x = threadIdx.x & 31u, y = threadIdx.x >> 5, e = blockIdx.x * 32u + x;
+  const uint32_t lo = a.blocks * y / 32u, hi = a.blocks * (y + 1u) / 32u;
+  uint32_t sum = 0;
+  if (e < a.experts) {
+#pragma unroll 8
+    for (uint32_t b = lo; b < hi; ++b) sum += __ldcg(a.counts + (size_t)b * a.experts + e);
+  }
+  sums[y][x] = sum;
+  __syncthreads();
+  if (e >= a.experts) return;
+  uint32_t before = 0;
+  for (uint32_t q = 0; q < y; ++q) before += sums[q][x];
+#pragma unroll 8
+  for (uint32_t b = lo; b < hi; ++b) {
+    uint32_t* at = a.counts + (size_t)b * a.experts + e;
+    const uint32_t c = __ldcg(at);
+    *at = before;
+    before += c;
+  }
+  if (y == 31u) a.counts[(size_t)a.blocks * a.experts + e] = before;
+}
+
+// Places the choices of each block.  Dynamic shared memory: places [experts], the bits of place_choices.
 __global__ void __launch_bounds__(1024) order_kernel(const RouteArgs a) {
   pdl_prologue();
   extern __shared__ uint32_t order_smem[];
   __shared__ uint32_t warp_total[32];
-  const uint32_t words = a.block_rows / 32u;
-  uint32_t *place = order_smem, *bits = place + a.experts, *sums = bits + a.experts * words;
-  const uint32_t lo = blockIdx.x * a.block_rows, hi = min(lo + a.block_rows, a.tokens);
+  const uint32_t words = (a.block_rows + 31u) / 32u;
+  uint32_t *place = order_smem, *bits = place + a.experts;
+  const uint32_t lo = blockIdx.x * a.block_rows, hi = min(lo + a.block_rows, a.tokens), e = threadIdx.x;
+  const uint32_t all = e < a.experts ? __ldcg(a.counts + (size_t)a.blocks * a.experts + e) : 0u;
+  const uint32_t earlier = e < a.experts ? __ldcg(a.counts + (size_t)blockIdx.x * a.experts + e) : 0u;
   for (uint32_t i = threadIdx.x; i < a.experts * words; i += blockDim.x) bits[i] = 0u;
-  // how many rows of all blocks, and of the blocks before this one, go to each expert: a.share threads add up an expert's counts
-  uint32_t carry = 0;
-  const uint32_t at_once = blockDim.x / a.share, part = threadIdx.x / at_once;
-  const uint32_t b_lo = a.blocks * part / a.share, b_hi = a.blocks * (part + 1u) / a.share;
-  for (uint32_t e0 = 0; e0 < a.experts; e0 += at_once) {
-    const uint32_t e = e0 + threadIdx.x % at_once;
-    uint32_t all = 0, before = 0;
-    if (e < a.experts) {
-#pragma unroll 8
-      for (uint32_t b = b_lo; b < b_hi; ++b) {
-        const uint32_t c = __ldcg(a.counts + (size_t)b * a.experts + e);
-        all += c;
-        before += b < blockIdx.x ? c : 0u;
-      }
-    }
-    sums[threadIdx.x] = all;
-    sums[blockDim.x + threadIdx.x] = before;
-    __syncthreads();
-    all = before = 0;
-    if (part == 0u && e < a.experts) {
-      for (uint32_t q = 0; q < a.share; ++q) {
-        all += sums[q * at_once + threadIdx.x];
-        before += sums[blockDim.x + q * at_once + threadIdx.x];
-      }
-    }
-    uint32_t total;
-    const uint32_t start = carry + sum_before(all, warp_total, total);
-    if (part == 0u && e < a.experts) {
-      place[e] = start + before;
-      if (blockIdx.x == 0u) a.offsets[e] = (int32_t)start;
-    }
-    carry += total;
+  uint32_t used;
+  const uint32_t start = sum_before(all, warp_total, used);      // (at most 1024 experts: a thread each)
+  if (e < a.experts) {
+    place[e] = start + earlier;
+    if (blockIdx.x == 0u) a.offsets[e] = (int32_t)start;
   }
-  if (blockIdx.x == 0u && threadIdx.x == 0u) a.offsets[a.experts] = (int32_t)carry;
+  if (blockIdx.x == 0u && threadIdx.x == 0u) a.offsets[a.experts] = (int32_t)used;
   __syncthreads();
   place_choices(a, lo, hi, place, bits, words);
   // behind the last
   const uint64_t end = (uint64_t)a.tokens * a.top_k;
-  for (uint64_t i = carry + (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < end; i += (uint64_t)gridDim.x * blockDim.x) a.order[i] = -1;
+  for (uint64_t i = used + (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < end; i += (uint64_t)gridDim.x * blockDim.x) a.order[i] = -1;
 }
 
 uint32_t rows_of_a_block(const psb_route_desc& d) {
-  // a block per SM, in whole words of the bit masks
-  uint32_t rows = round_up((d.tokens + kSms - 1u) / kSms, 32u);
-  return rows < kMaxBlockRows ? rows : kMaxBlockRows;
+  // a block per SM
+  const uint32_t rows = (d.tokens + kSms - 1u) / kSms;
+  return rows < 32u ? 32u : rows < kMaxBlockRows ? rows : kMaxBlockRows;
 }
 
 // ---- combine -------------------------------------------------------------------------------------------------------------
@@ -506,33 +552,39 @@ struct CombineArgs {
   void* out;
   uint32_t* err;
   uint32_t tokens, top_k, n, rows, chunks, wide;   // chunks: pieces of 16 input bytes in a row
+  uint32_t row_blocks, threads;                    // blocks for a row, their threads
   uint64_t y_stride, out_stride;
 };
 
 // A thread owns 16 input bytes of an output row; the rows of up to eight choices are loaded together.
 template <typename TI, typename TO>
-__global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a) {
+__global__ void __launch_bounds__(256, 4) combine_kernel(const CombineArgs a) {
   pdl_prologue();
   constexpr int kPer = 16 / sizeof(TI);
-  const uint64_t total = (uint64_t)a.tokens * a.chunks;
-  for (uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (uint64_t)gridDim.x * blockDim.x) {
-    const uint32_t t = (uint32_t)(i / a.chunks), c = (uint32_t)(i - (uint64_t)t * a.chunks) * kPer;
+  const uint32_t t = blockIdx.x / a.row_blocks, piece = (blockIdx.x - t * a.row_blocks) * blockDim.x + threadIdx.x;
+  if (piece < a.chunks) {
+    const uint32_t c = piece * kPer;
     const bool whole = a.wide && c + kPer <= a.n;
     float sum[kPer];
 #pragma unroll
     for (int e = 0; e < kPer; ++e) sum[e] = 0.0f;
     for (uint32_t j0 = 0; j0 < a.top_k; j0 += 8u) {
+      // all places and weights first: a row's address waits for its place, and must not hold up the next place
       uint4 v[8];
       float w[8];
+      int s[8];
       bool on[8];
 #pragma unroll
       for (uint32_t j = 0; j < 8u; ++j) {
         const bool there = j0 + j < a.top_k;
-        const int s = there ? a.slot[(size_t)t * a.top_k + j0 + j] : -1;
-        if (s >= 0 && (uint32_t)s >= a.rows) atomicOr(a.err, kDevErrRange);
-        on[j] = s >= 0 && (uint32_t)s < a.rows;
-        w[j] = on[j] ? a.weights[(size_t)t * a.top_k + j0 + j] : 0.0f;
-        const TI* row = (const TI*)a.y + (on[j] ? (uint64_t)s : 0u) * a.y_stride + c;
+        s[j] = there ? a.slot[(size_t)t * a.top_k + j0 + j] : -1;
+        w[j] = there ? a.weights[(size_t)t * a.top_k + j0 + j] : 0.0f;
+      }
+#pragma unroll
+      for (uint32_t j = 0; j < 8u; ++j) {
+        on[j] = s[j] >= 0 && (uint32_t)s[j] < a.rows;
+        if (s[j] >= 0 && !on[j]) atomicOr(a.err, kDevErrRange);
+        const TI* row = (const TI*)a.y + (on[j] ? (uint64_t)s[j] : 0u) * a.y_stride + c;
         if (whole) {
           if (on[j]) v[j] = *reinterpret_cast<const uint4*>(row);
         } else {
@@ -570,8 +622,7 @@ __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a) {
 
 template <typename TI, typename TO>
 void launch_combine_as(const CombineArgs& a, cudaStream_t s) {
-  const uint64_t want = ((uint64_t)a.tokens * a.chunks + 255u) / 256u;
-  launch_pdl(combine_kernel<TI, TO>, (uint32_t)(want < kSms * 64u ? want : kSms * 64u), 256, 0, s, a);
+  launch_pdl(combine_kernel<TI, TO>, a.tokens * a.row_blocks, a.threads, 0, s, a);
 }
 template <typename TI>
 void launch_combine_from(const CombineArgs& a, uint32_t out_dtype, cudaStream_t s) {
@@ -584,7 +635,7 @@ void launch_combine_from(const CombineArgs& a, uint32_t out_dtype, cudaStream_t 
 
 size_t route_scratch_bytes(const psb_route_desc& d) {
   const uint32_t rows = rows_of_a_block(d);
-  return (size_t)((d.tokens + rows - 1u) / rows) * d.experts * sizeof(uint32_t);
+  return (size_t)((d.tokens + rows - 1u) / rows + 1u) * d.experts * sizeof(uint32_t);      // and the sums
 }
 
 cudaError_t launch_route(const void* logits, const float* bias, const uint8_t* mask, const psb_route_desc& d, int32_t* ids,
@@ -618,11 +669,9 @@ cudaError_t launch_route(const void* logits, const float* bias, const uint8_t* m
   while (el * 32u < d.experts) el *= 2u;
   const uint32_t size = d.experts / d.groups, lanes = size / el;
   a.lanes_per_group = size % el == 0u && (lanes & (lanes - 1u)) == 0u ? lanes : 0u;
-  a.share = 1;
-  while (a.share < 32u && a.share * 2u * d.experts <= 1024u) a.share *= 2u;
-  const uint32_t ints = d.experts * (a.alone ? 1u + a.block_rows / 32u : 1u);
+  const uint32_t ints = d.experts * (a.alone ? 1u + (a.block_rows + 31u) / 32u : 1u);
   auto go = [&](auto kernel, uint32_t threads) {
-    const size_t smem = ((ints * 4u + 15u) & ~15u) + (d.groups > 1u ? sizeof(double) * (threads / 32u) * (d.experts + d.groups) : 0u);
+    const size_t smem = ((ints * 4u + 15u) & ~15u) + sizeof(double) * (threads / 32u) * (d.experts + d.groups);
     if (smem > 48u * 1024u) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     launch_pdl(kernel, a.blocks, threads, smem, s, a);
   };
@@ -634,7 +683,9 @@ cudaError_t launch_route(const void* logits, const float* bias, const uint8_t* m
   else go(route_kernel<32>, kRouteThreads<32>);
   note_launch();
   if (order && !a.alone) {
-    const size_t bytes = sizeof(uint32_t) * (d.experts * (1u + a.block_rows / 32u) + 2048u);
+    const size_t bytes = sizeof(uint32_t) * d.experts * (1u + (a.block_rows + 31u) / 32u);
+    launch_pdl(scan_kernel, (d.experts + 31u) / 32u, 1024, 0, s, a);
+    note_launch();
     if (bytes > 48u * 1024u) cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     launch_pdl(order_kernel, a.blocks, 1024, bytes, s, a);
     note_launch();
@@ -658,6 +709,8 @@ cudaError_t launch_combine(const void* y, const float* weights, const int32_t* s
   a.out_stride = d.out_stride;
   const uint32_t in = d.in_dtype == PSB_DT_F32 ? 4u : 2u, to = d.out_dtype == PSB_DT_F32 ? 4u : 2u;
   a.chunks = (d.n + 16u / in - 1u) / (16u / in);
+  a.threads = a.chunks < 256u ? round_up(a.chunks, 32u) : 256u;
+  a.row_blocks = (a.chunks + a.threads - 1u) / a.threads;
   a.wide = (((uintptr_t)y | (uintptr_t)out | d.y_stride * in | d.out_stride * to) & 15u) == 0u;
   if (d.in_dtype == PSB_DT_F32) launch_combine_from<float>(a, d.out_dtype, s);
   else if (d.in_dtype == PSB_DT_BF16) launch_combine_from<__nv_bfloat16>(a, d.out_dtype, s);

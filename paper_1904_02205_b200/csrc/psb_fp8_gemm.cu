@@ -209,7 +209,7 @@ template <> __device__ __forceinline__ __nv_bfloat16 round_to<__nv_bfloat16>(flo
 template <> __device__ __forceinline__ __half round_to<__half>(float v) { return __float2half_rn(v); }
 
 __device__ __forceinline__ float finish(float y, const float* bias, uint32_t relu) {
-  if (bias) y += __ldcg(bias);
+  if (bias) y += __ldca(bias);
   return relu && y < 0.0f ? 0.0f : y;
 }
 
@@ -734,9 +734,10 @@ __global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs g) {
   const uint32_t rows = used < 0 ? 0u : min((uint32_t)used, g.rows);
   // pieces of codes, then one of scales per block of 128 pieces' row
   const uint32_t per_row = g.pieces + (g.k_blocks + 3u) / 4u;
-  const uint64_t total = (uint64_t)rows * per_row;
-  for (uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (uint64_t)gridDim.x * blockDim.x) {
-    const uint32_t r = (uint32_t)(i / per_row), c = (uint32_t)(i - (uint64_t)r * per_row);
+  const uint32_t i0 = blockIdx.x * blockDim.x + threadIdx.x, stride = gridDim.x * blockDim.x;
+  const uint32_t step_r = stride / per_row, step_c = stride - step_r * per_row;
+  uint32_t r = i0 / per_row, c = i0 - r * per_row;
+  for (; r < rows; r += step_r) {
     const int o = __ldcg(g.order + r);
     if (c == 0u && (o < 0 || (uint32_t)o >= g.m)) atomicOr(g.err, kDevErrRange);
     const uint64_t from = o < 0 ? 0u : min((uint32_t)o, g.m - 1u);
@@ -750,6 +751,8 @@ __global__ void __launch_bounds__(256) gather_rows_kernel(const GatherArgs g) {
       for (uint32_t b = (c - g.pieces) * 4u; b < min((c - g.pieces) * 4u + 4u, g.k_blocks); ++b)
         g.scale_to[(uint64_t)r * g.k_blocks + b] = g.scale[from * g.scale_stride + b];
     }
+    c += step_c;
+    if (c >= per_row) { c -= per_row; ++r; }
   }
 }
 

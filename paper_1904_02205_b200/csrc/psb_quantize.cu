@@ -95,9 +95,10 @@ template <typename T, bool E5M2>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const QuantArgs a) {
   pdl_prologue();
   const uint32_t sub = threadIdx.x & 7u;
-  const uint64_t total = (uint64_t)a.rows * a.blocks;
-  for (uint64_t i = (blockIdx.x * 256u + threadIdx.x) >> 3; i < total; i += gridDim.x * 32u) {
-    const uint32_t r = (uint32_t)(i / a.blocks), b = (uint32_t)(i - (uint64_t)r * a.blocks);
+  // (a division a thread, not one a block of values: in 64 bits they took a third of the time)
+  const uint32_t i0 = (blockIdx.x * 256u + threadIdx.x) >> 3, step_r = gridDim.x * 32u / a.blocks, step_b = gridDim.x * 32u - step_r * a.blocks;
+  uint32_t r = i0 / a.blocks, b = i0 - r * a.blocks;
+  for (; r < a.rows; r += step_r) {
     float v[16];
     const uint32_t c = b * 128u + sub * 16u;
     load16<T>((const T*)a.x + r * a.x_stride, c, a.cols, a.wide_in, v);
@@ -108,6 +109,8 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const QuantArgs a) {
     const Scale s = scale_of(m, a.top);
     if (sub == 0u) a.scales[r * a.scale_stride + b] = s.scale;
     store16<E5M2>(a.codes + r * a.code_stride, c, a.cols, a.wide_out, v, s.inverse);
+    b += step_b;
+    if (b >= a.blocks) { b -= a.blocks; ++r; }
   }
 }
 
