@@ -114,10 +114,23 @@ __device__ __forceinline__ void load_logits(const RouteArgs& a, uint32_t t, uint
   for (int i = 0; i < EL; ++i) x[i] = clean(x[i]);
 }
 
-// Whether two experts of a row have the same logit and the same bias (a look at memory: the registers are another lane's).
-__device__ __noinline__ bool same_select(const RouteArgs& a, uint32_t t, uint32_t e, uint32_t o) {
-  return load_logit(a, (uint64_t)t * a.logit_stride + e) == load_logit(a, (uint64_t)t * a.logit_stride + o) &&
-         (!a.bias || __ldca(a.bias + e) == __ldca(a.bias + o));
+// Two experts of a row, e chosen before o by fp32 values: 1 if that is right, -1 if the other way round is, 0 if it takes the whole row.
+__device__ __noinline__ int exact_order(const RouteArgs& a, uint32_t t, uint32_t e, uint32_t o) {
+  const uint64_t row = (uint64_t)t * a.logit_stride;
+  const float x = load_clean(a, row + e), y = load_clean(a, row + o);
+  const float b = a.bias ? __ldca(a.bias + e) : 0.0f, c = a.bias ? __ldca(a.bias + o) : 0.0f;
+  const int by_index = e < o ? 1 : -1;
+  if (b == c && x == y) return by_index;
+  if (!a.bias) {
+    if (x > y) return 1;
+    if (!a.sigmoid) return -1;
+  } else if (!a.sigmoid) {
+    return 0;
+  }
+  double v[2];
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i) v[i] = 1.0 / (1.0 + exp(-(double)(i ? y : x))) + (double)(i ? c : b);
+  return v[0] > v[1] ? 1 : v[0] < v[1] ? -1 : by_index;
 }
 
 // The two largest keys of a run of experts, put together with those of another run.
@@ -246,8 +259,8 @@ __device__ __forceinline__ bool choose(const RouteArgs& a, const float (&x)[EL],
   uint32_t taken = 0;          // bit i: my expert i
   my_id = -1;
   int my_key = kNone;
-  // one round more than there are choices: is the last choice certain against the first that is left out
-  const uint32_t rounds = a.top_k + (by_logit || a.top_k == 32u ? 0u : 1u);
+  // two rounds more than there are choices: is the last choice certain against the first that is left out
+  const uint32_t rounds = a.top_k + (by_logit || a.top_k > 30u ? 0u : 2u);
   for (uint32_t j = 0; j < rounds; ++j) {
     const int top = warp_max(best);
     if (top == kNone) break;
@@ -267,12 +280,27 @@ __device__ __forceinline__ bool choose(const RouteArgs& a, const float (&x)[EL],
     }
   }
   if (!by_logit) {
-    // each choice against the next (equal logits under equal biases are equal)
+    // each choice against the next
     const int other = __shfl_down_sync(kAll, my_key, 1), other_id = __shfl_down_sync(kAll, my_id, 1);
     const float v = value_of(my_key), w = value_of(other);
-    if (lane < a.top_k && lane < 31u && my_id >= 0 && other_id >= 0 && !(v - w > unit + kRound * (fabsf(v) + fabsf(w))))
-      sure = sure && same_select(a, t, (uint32_t)my_id, (uint32_t)other_id);
-    if (a.top_k == 32u) sure = false;           // (no lane for the first that is left out)
+    const bool pair = lane < 31u && my_id >= 0 && other_id >= 0 && lane <= a.top_k;
+    const uint32_t doubts = __ballot_sync(kAll, pair && !(v - w > unit + kRound * (fabsf(v) + fabsf(w))));
+    if (doubts) {
+      // Pairs that are right as they stand settle everything between the first and the last of them.  One that is not is turned round
+      // if its neighbours are certain.  Two in doubt at the border: others behind them may be as close, so the whole row is done again.
+      bool swap = false;
+      if (((doubts >> lane) & 1u) && lane < a.top_k) {
+        const int order = exact_order(a, t, (uint32_t)my_id, (uint32_t)other_id);
+        swap = order < 0;
+        const bool border = lane == a.top_k - 1u && ((doubts >> lane >> 1) & 1u);
+        if (order == 0 || border || (swap && (((doubts >> 1) | (doubts << 1)) >> lane & 1u))) sure = false;
+      }
+      const uint32_t swaps = __ballot_sync(kAll, swap);
+      const int above = __shfl_up_sync(kAll, my_id, 1);
+      if ((swaps >> lane) & 1u) my_id = other_id;
+      else if (lane && ((swaps >> (lane - 1u)) & 1u)) my_id = above;
+    }
+    if (a.top_k > 30u) sure = false;           // (no lanes for those that are left out)
   }
   if (lane >= a.top_k) my_id = -1;
   return __all_sync(kAll, sure);
