@@ -16,13 +16,6 @@ namespace psb {
 
 namespace {
 
-template <typename T> __device__ __forceinline__ float to_f32(T v);
-template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <> __device__ __forceinline__ float to_f32<__half>(__half v) { return __half2float(v); }
-
-__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
-
 struct Scale {
   float scale, inverse;
 };
@@ -35,48 +28,98 @@ __device__ __forceinline__ Scale scale_of(float amax, float top) {
 
 template <bool E5M2>
 __device__ __forceinline__ uint32_t codes2(float a, float b) {
-  // (infinities as NaN: inf - inf)
-  const float2 v = {finite(a) ? a : a - a, finite(b) ? b : b - b};
-  return (uint32_t)__nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, E5M2 ? __NV_E5M2 : __NV_E4M3);
+  return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, E5M2 ? __NV_E5M2 : __NV_E4M3);
 }
+
+// Values as they come, 4 / sizeof(T) in a word.  Without their signs they are ordered as whole numbers, infinities and NaN
+// behind the finite ones: the largest of a block tells whether there are any, and only then is each value asked.
+template <typename T> struct Words;
+template <> struct Words<float> {
+  static constexpr uint32_t kInf = 0x7F800000u;
+  static __device__ __forceinline__ uint32_t max_of(uint32_t m, uint32_t w) { return max(m, w & 0x7FFFFFFFu); }
+  static __device__ __forceinline__ uint32_t whole(uint32_t m) { return m; }
+  static __device__ __forceinline__ float value(uint32_t bits) { return __uint_as_float(bits); }
+  template <int N> static __device__ __forceinline__ float get(const uint32_t (&w)[N], int j) { return __uint_as_float(w[j]); }
+};
+struct HalfWords {
+  static __device__ __forceinline__ uint32_t max_of(uint32_t m, uint32_t w) { return __vmaxu2(m, w & 0x7FFF7FFFu); }
+  static __device__ __forceinline__ uint32_t whole(uint32_t m) { return max(m & 0xFFFFu, m >> 16); }
+};
+template <> struct Words<__nv_bfloat16> : HalfWords {
+  static constexpr uint32_t kInf = 0x7F80u;
+  static __device__ __forceinline__ float value(uint32_t bits) { return __uint_as_float(bits << 16); }
+  template <int N> static __device__ __forceinline__ float get(const uint32_t (&w)[N], int j) {
+    return __uint_as_float(j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+  }
+};
+template <> struct Words<__half> : HalfWords {
+  static constexpr uint32_t kInf = 0x7C00u;
+  static __device__ __forceinline__ float value(uint32_t bits) { return __half2float(__ushort_as_half((uint16_t)bits)); }
+  template <int N> static __device__ __forceinline__ float get(const uint32_t (&w)[N], int j) { return value(w[j / 2] >> (j & 1 ? 16 : 0) & 0xFFFFu); }
+};
+template <typename T> constexpr int kWords = 4 * (int)sizeof(T);      // of 16 values
+
+__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
 
 // 16 consecutive values of a row, from column c on; zeros behind the row's end.
 template <typename T>
-__device__ __forceinline__ void load16(const T* row, uint32_t c, uint32_t cols, bool wide, float (&v)[16]) {
-  constexpr int kPer = 16 / sizeof(T);
+__device__ __forceinline__ void load16(const T* row, uint32_t c, uint32_t cols, bool wide, uint32_t (&w)[kWords<T>]) {
   if (wide && c + 16u <= cols) {
 #pragma unroll
-    for (int i = 0; i < 16 / kPer; ++i) {
-      const uint4 w = *reinterpret_cast<const uint4*>(row + c + i * kPer);
-      const T* t = reinterpret_cast<const T*>(&w);
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) v[i * kPer + j] = to_f32<T>(t[j]);
+    for (int i = 0; i < kWords<T> / 4; ++i) {
+      const uint4 q = *reinterpret_cast<const uint4*>(row + c + i * (16 / (int)sizeof(T)));
+      w[4 * i] = q.x;
+      w[4 * i + 1] = q.y;
+      w[4 * i + 2] = q.z;
+      w[4 * i + 3] = q.w;
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = c + j < cols ? to_f32<T>(row[c + j]) : 0.0f;
+    for (int i = 0; i < kWords<T>; ++i) w[i] = 0u;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      if (c + j >= cols) continue;
+      if (sizeof(T) == 4) w[j] = reinterpret_cast<const uint32_t*>(row)[c + j];
+      else w[j / 2 % kWords<T>] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[c + j] << (j & 1 ? 16 : 0);
+    }
   }
 }
 
-template <bool E5M2>
-__device__ __forceinline__ void store16(uint8_t* row, uint32_t c, uint32_t cols, bool wide, const float (&v)[16], float inverse) {
-  uint32_t w[4];
+template <typename T, bool E5M2>
+__device__ __forceinline__ void store16(uint8_t* row, uint32_t c, uint32_t cols, bool wide, const uint32_t (&w)[kWords<T>], float inverse, bool all_finite) {
+  uint32_t q[4];
+  float v[16];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    w[i] = codes2<E5M2>(v[4 * i] * inverse, v[4 * i + 1] * inverse) | codes2<E5M2>(v[4 * i + 2] * inverse, v[4 * i + 3] * inverse) << 16;
+  for (int j = 0; j < 16; ++j) v[j] = Words<T>::get(w, j) * inverse;
+  if (!all_finite) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = finite(v[j]) ? v[j] : NAN;      // (a finite value times the reciprocal is finite)
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i] = codes2<E5M2>(v[4 * i], v[4 * i + 1]) | codes2<E5M2>(v[4 * i + 2], v[4 * i + 3]) << 16;
   if (wide && c + 16u <= cols) {
-    *reinterpret_cast<uint4*>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    *reinterpret_cast<uint4*>(row + c) = make_uint4(q[0], q[1], q[2], q[3]);
   } else {
 #pragma unroll
     for (int j = 0; j < 16; ++j)
-      if (c + j < cols) row[c + j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
+      if (c + j < cols) row[c + j] = (uint8_t)(q[j >> 2] >> (8 * (j & 3)));
   }
 }
 
-__device__ __forceinline__ float max16(const float (&v)[16]) {
-  float m = 0.0f;
+template <typename T>
+__device__ __forceinline__ uint32_t max16(uint32_t m, const uint32_t (&w)[kWords<T>]) {
 #pragma unroll
-  for (int j = 0; j < 16; ++j) m = fmaxf(m, finite(v[j]) ? fabsf(v[j]) : 0.0f);
+  for (int i = 0; i < kWords<T>; ++i) m = Words<T>::max_of(m, w[i]);
+  return m;
+}
+// Of the finite values alone (the rare case).
+template <typename T>
+__device__ __forceinline__ float finite16(float m, const uint32_t (&w)[kWords<T>]) {
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const float v = fabsf(Words<T>::get(w, j));
+    m = finite(v) ? fmaxf(m, v) : m;
+  }
   return m;
 }
 
@@ -99,16 +142,23 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const QuantArgs a) {
   const uint32_t i0 = (blockIdx.x * 256u + threadIdx.x) >> 3, step_r = gridDim.x * 32u / a.blocks, step_b = gridDim.x * 32u - step_r * a.blocks;
   uint32_t r = i0 / a.blocks, b = i0 - r * a.blocks;
   for (; r < a.rows; r += step_r) {
-    float v[16];
     const uint32_t c = b * 128u + sub * 16u;
-    load16<T>((const T*)a.x + r * a.x_stride, c, a.cols, a.wide_in, v);
-    float m = max16(v);
+    uint32_t w[kWords<T>];
+    load16<T>((const T*)a.x + r * a.x_stride, c, a.cols, a.wide_in, w);
+    uint32_t m = Words<T>::whole(max16<T>(0u, w));
     const uint32_t peers = 0xFFu << (threadIdx.x & 24u);
 #pragma unroll
-    for (int d = 4; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(peers, m, d));
-    const Scale s = scale_of(m, a.top);
+    for (int d = 4; d > 0; d >>= 1) m = max(m, __shfl_xor_sync(peers, m, d));
+    float amax = Words<T>::value(m);
+    const bool all_finite = m < Words<T>::kInf;
+    if (!all_finite) {
+      amax = finite16<T>(0.0f, w);
+#pragma unroll
+      for (int d = 4; d > 0; d >>= 1) amax = fmaxf(amax, __shfl_xor_sync(peers, amax, d));
+    }
+    const Scale s = scale_of(amax, a.top);
     if (sub == 0u) a.scales[r * a.scale_stride + b] = s.scale;
-    store16<E5M2>(a.codes + r * a.code_stride, c, a.cols, a.wide_out, v, s.inverse);
+    store16<T, E5M2>(a.codes + r * a.code_stride, c, a.cols, a.wide_out, w, s.inverse, all_finite);
     b += step_b;
     if (b >= a.blocks) { b -= a.blocks; ++r; }
   }
@@ -118,30 +168,43 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const QuantArgs a) {
 template <typename T, bool E5M2>
 __global__ void __launch_bounds__(256) quantize_tile_kernel(const QuantArgs a) {
   pdl_prologue();
-  __shared__ float part[8];
+  __shared__ uint32_t part[8];
   const uint32_t b = blockIdx.x % a.blocks, rb = blockIdx.x / a.blocks;
   const uint32_t c = b * 128u + (threadIdx.x & 7u) * 16u, r0 = rb * 128u + (threadIdx.x >> 3);
-  float v[4][16];
-  float m = 0.0f;
+  uint32_t w[4][kWords<T>];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t r = r0 + 32u * i;
-    load16<T>((const T*)a.x + r * a.x_stride, c, r < a.rows ? a.cols : 0u, a.wide_in, v[i]);
+    load16<T>((const T*)a.x + r * a.x_stride, c, r < a.rows ? a.cols : 0u, a.wide_in, w[i]);
   }
+  uint32_t m = 0u;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) m = fmaxf(m, max16(v[i]));
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+  for (int i = 0; i < 4; ++i) m = max16<T>(m, w[i]);
+  m = __reduce_max_sync(0xFFFFFFFFu, Words<T>::whole(m));
   if ((threadIdx.x & 31u) == 0u) part[threadIdx.x >> 5] = m;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, part[i]);
-  const Scale s = scale_of(m, a.top);
+  for (int i = 0; i < 8; ++i) m = max(m, part[i]);
+  float amax = Words<T>::value(m);
+  const bool all_finite = m < Words<T>::kInf;        // (the same for the whole block of threads)
+  if (!all_finite) {
+    amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) amax = finite16<T>(amax, w[i]);
+    // (numbers that are not negative are ordered as their bits)
+    const uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax));
+    __syncthreads();
+    if ((threadIdx.x & 31u) == 0u) part[threadIdx.x >> 5] = bits;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, __uint_as_float(part[i]));
+  }
+  const Scale s = scale_of(amax, a.top);
   if (threadIdx.x == 0u) a.scales[rb * a.scale_stride + b] = s.scale;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t r = r0 + 32u * i;
-    if (r < a.rows) store16<E5M2>(a.codes + r * a.code_stride, c, a.cols, a.wide_out, v[i], s.inverse);
+    if (r < a.rows) store16<T, E5M2>(a.codes + r * a.code_stride, c, a.cols, a.wide_out, w[i], s.inverse, all_finite);
   }
 }
 
