@@ -886,7 +886,9 @@ psb_status psb_combine_experts(psb_ctx* ctx, const void* y_dev, const float* wei
   if (!row_stride(d.y_stride, d.n) || !row_stride(d.out_stride, d.n)) return PSB_ERR_INVALID_ARG;
   if (misaligned(y_dev, size_of(d.in_dtype)) || misaligned(out_dev, size_of(d.out_dtype)) || misaligned(weights_dev, 4) || misaligned(slot_dev, 4))
     return PSB_ERR_INVALID_ARG;
-  if (d.top_k > 32u || d.n >= (1u << 31) || d.rows >= (1u << 31) || (uint64_t)d.tokens * d.top_k >= (1ull << 31)) return PSB_ERR_UNSUPPORTED;
+  if (d.top_k > 32u || d.n >= (1u << 31) || d.rows >= (1u << 31) || (uint64_t)d.tokens * d.top_k >= (1ull << 31) ||
+      (uint64_t)d.tokens * ((d.n + 127u) / 128u) >= (1ull << 31))
+    return PSB_ERR_UNSUPPORTED;
   cudaSetDevice(ctx->device);
   return launch_combine(y_dev, weights_dev, slot_dev, d, out_dev, ctx->err_dev, (cudaStream_t)stream) == cudaSuccess ? PSB_OK : PSB_ERR_CUDA;
 }
