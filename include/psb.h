@@ -417,7 +417,8 @@ psb_status psb_sample_level_static(const float* w_dev, const psb_wshape* shape,
  * elements apart (0: as many as a row has; blocks of a scale row likewise).  Strides may exceed the row; what
  * lies between rows is neither read nor written.  Scratch is taken by psb_route_experts (counts) and, with an order, by
  * psb_gemm_fp8_experts (the rows in that order), see the
- * top of this file.  They run on the context's device, which becomes the current one. */
+ * top of this file.  They run on the context's device, which becomes the current one.  Waits inside their kernels are
+ * bounded by a number of polls, a 256th of psb_set_wait_limit's clocks (a poll takes from 20 clocks to microseconds). */
 
 /* Codes and scales of a matrix.  Per block of block_rows x 128 (1: activations, 128: filters; blocks at the ends are
  * cut off):

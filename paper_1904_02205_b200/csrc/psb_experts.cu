@@ -5,9 +5,10 @@
 // scores are monotone in the logits and the logits themselves are compared; otherwise fp32 values decide wherever
 // they are further apart than their error bound (kRound), and the row is done again in 64 bits where they are not (equal
 // logits with equal biases are equal, and need no second look).
-// The order of the choices is a counting sort: blocks of consecutive rows count their choices per expert; the
-// second launch adds up the counts of the blocks before it and places its own, the rank inside a block being the number of
+// The order of the choices is a counting sort: blocks of consecutive rows count their choices per expert, a second launch
+// sums the counts of the blocks before each, a third places the choices, the rank inside a block being the number of
 // earlier rows that chose the same expert (bit masks over the block's rows).  Nothing depends on the order of atomics.
+// Up to 64 rows one block does all three.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -557,9 +558,9 @@ __global__ void __launch_bounds__(1024) order_kernel(const RouteArgs a) {
 }
 
 uint32_t rows_of_a_block(const psb_route_desc& d) {
-  // a block per SM
+  // a block per SM; up to 64 rows one block alone, which spares two launches (4 us of the host's time)
   const uint32_t rows = (d.tokens + kSms - 1u) / kSms;
-  return rows < 32u ? 32u : rows < kMaxBlockRows ? rows : kMaxBlockRows;
+  return rows < 64u ? 64u : rows < kMaxBlockRows ? rows : kMaxBlockRows;
 }
 
 // ---- combine -------------------------------------------------------------------------------------------------------------

@@ -159,7 +159,7 @@ def test_rows_whose_mask_leaves_little_or_nothing(ctx, score, with_bias, groups)
     check_route(ctx, x, 5, score, bias, groups, 2 if groups > 1 else 1, 2, mask=np.zeros(12, np.uint8))
 
 
-@pytest.mark.parametrize("tokens", [1, 31, 32, 33, 149, 4736, 4737, 9000])
+@pytest.mark.parametrize("tokens", [1, 31, 32, 33, 64, 65, 149, 4736, 4737, 9000])
 def test_order_over_many_blocks(ctx, tokens):
     rng = np.random.default_rng(tokens)
     x = rng.normal(0, 1, size=(tokens, 16)).astype(np.float32)
@@ -178,6 +178,23 @@ def test_order_of_very_many_rows(ctx):
     assert torch.equal(got["order"].long(), by // k)
     assert torch.equal(got["slot"].reshape(-1).long()[by], torch.arange(T * k, device="cuda"))
     assert torch.equal(got["offsets"][1:].long(), torch.bincount(ids.reshape(-1), minlength=E).cumsum(0))
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,top_k,groups,group_best", [(48, 3, 1, 1), (64, 30, 1, 1), (64, 31, 1, 1), (256, 8, 8, 2), (64, 8, 4, 1), (512, 7, 1, 1)])
+def test_rows_of_pairs_that_are_nearly_equal(ctx, score, experts, top_k, groups, group_best):
+    """Rows that differ from one another by less than fp32 resolves, under a bias that makes them flat; and without one."""
+    rng = np.random.default_rng(experts + top_k)
+    x0 = rng.normal(0, 1, size=experts)
+    p = np.exp(x0.astype(np.float32).astype(np.float64))
+    p = p / p.sum() if score == "softmax" else p / (1 + p)
+    bias = (0.5 - p).astype(np.float32)
+    for step in (1e-7, 1e-6, 1e-4):
+        x = (x0[None] + step * rng.normal(size=(64, experts))).astype(np.float32)
+        check_route(ctx, x, top_k, score, bias, groups, max(1, groups // 2), group_best)
+        y = np.sort(x, axis=1)
+        y[:, 1::2] = np.nextafter(y[:, ::2], np.inf)
+        check_route(ctx, y, top_k, score, None, groups, max(1, groups // 2), group_best)
 
 
 def test_strided_logits_and_no_order(ctx):

@@ -180,3 +180,42 @@ def test_captured_and_replayed_on_other_streams(ctx):
         other = layer(side)
     side.synchronize()
     assert torch.equal(other, got) and not torch.equal(want, got)
+
+
+def test_outputs_beyond_32_bits(ctx):
+    """Byte offsets of more than 32 bits in the values, the codes and the product."""
+    m, n, k = 66000, 33100, 72
+    rng = np.random.default_rng(7)
+    a, b = codes(rng, m, k), codes(rng, n, k)
+    sa, sb = scales(rng, m, 1), scales(rng, up(n, 128), 1)
+    y = ctx.gemm_fp8(a, sa, b, sb)
+    ctx.check_device()
+    assert y.numel() * 2 > 1 << 32
+    for rows in (slice(0, 40), slice(32700, 32800), slice(m - 50, m)):
+        check_product(y[rows], *product(a[rows], sa[rows], b, sb), k)
+    got, scale = ctx.quantize_fp8(y)
+    for rows in (slice(0, 3), slice(m - 3, m)):
+        want, want_scale = quantise(y[rows], 1, E4)
+        assert torch.equal(scale[rows].cpu(), want_scale)
+        same_codes(got[rows], want)
+    del got, scale
+    w = torch.full((2, 2), 0.5, device="cuda")
+    out = ctx.combine_experts(y, w, torch.tensor([[0, m - 1], [m - 1, m - 2]], dtype=torch.int32, device="cuda"), out_dtype=torch.float32)
+    assert torch.equal(out[0], 0.5 * y[0].float() + 0.5 * y[m - 1].float()) and torch.equal(out[1], 0.5 * y[m - 1].float() + 0.5 * y[m - 2].float())
+
+
+@pytest.mark.parametrize("m", [40, 500])
+def test_two_streams_at_once(ctx, m):
+    rng = np.random.default_rng(m)
+    a, b = codes(rng, m, 1024), codes(rng, 600, 1024)
+    sa, sb = scales(rng, m, 8), scales(rng, 5, 8)
+    want = ctx.gemm_fp8(a, sa, b, sb)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        got = []
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append(ctx.gemm_fp8(a, sa, b, sb))
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, want) for g in got)
