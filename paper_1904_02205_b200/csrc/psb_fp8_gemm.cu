@@ -20,14 +20,14 @@ constexpr uint32_t kFirstSumWarp = 4;          // before it: copies of a, MMA, c
 constexpr uint32_t kSumWarps = 8;              // warp & 3: quarter of the rows (of the TMEM lanes); upper four: second half of the columns
 constexpr uint32_t kGemmThreads = 32 * (kFirstSumWarp + kSumWarps);
 
-constexpr uint32_t kStageOutBytes = 2048;      // per epilogue warp: 32 rows x 64 bytes of output
+constexpr uint32_t kSlotBytes = 2048;          // 32 rows x 64 bytes of output, on their way from an epilogue warp to memory
 constexpr uint32_t kBandTiles = 8;             // row tiles that are walked together, so that filter tiles are met again in L2
 constexpr uint32_t kMaxRing = 8;
 constexpr uint32_t kScaleBlocks = 8;           // blocks of scales that are handed over together, twice buffered
 constexpr uint32_t kScaleRow = kRowsCta + 4;   // floats between blocks: eight lanes that write one row's blocks meet eight banks
 
 struct GemmMaps {
-  CUtensorMap a, b;
+  CUtensorMap a, b, out;     // out: boxes of a slot (where its rows start at multiples of 16 bytes)
 };
 
 struct GemmParams {
@@ -213,16 +213,27 @@ __device__ __forceinline__ float finish(float y, const float* bias, uint32_t rel
   return relu && y < 0.0f ? 0.0f : y;
 }
 
-// A warp's 32 rows (a row a lane) of NC columns leave through shared memory, 64 bytes of a row at a time: four lanes then
-// store what is contiguous.  `rows`: rows of these 32 that exist; `cols`: columns that exist from the first one on.
-template <typename T, int NC>
-__device__ __forceinline__ void store_rows(const GemmParams& p, const float (&acc)[NC], uint8_t* stage, uint64_t row0,
+// A warp's 32 rows (a row a lane) of NC columns leave through shared memory, 64 bytes of a row at a time.  Whole boxes of 32 rows are
+// taken by the copy engine (its 64-byte swizzle is the order that keeps the lanes' 16-byte pieces in different banks), so that
+// the warp is back at its sums while they drain: all SMs store at the same time.  `rows`: rows of these 32 that exist; `cols`:
+// columns that exist from the first one on.
+template <typename T, int NC, uint32_t kSlots>
+__device__ __forceinline__ void store_rows(const GemmMaps& maps, const GemmParams& p, const float (&acc)[NC], uint8_t* slots, uint64_t row0,
                                            uint32_t rows, uint32_t col0, uint32_t cols, const float* bias, uint32_t lane) {
-  constexpr uint32_t kCols = 64 / sizeof(T), kPer = 16 / sizeof(T);
+  constexpr uint32_t kCols = 64 / sizeof(T);
   T* out = (T*)p.g.out;
 #pragma unroll
   for (uint32_t c0 = 0; c0 < (uint32_t)NC; c0 += kCols) {
     if (c0 < cols) {               // (the same for the whole warp)
+      // (the engine cuts a box at the end of a row to pieces of 16 bytes, not to elements)
+      const bool boxes = p.wide_out && rows == 32u && c0 + kCols <= cols;
+      uint8_t* stage = slots + (boxes ? c0 / kCols % kSlots * kSlotBytes : 0u);
+      // the slot's last box has been read
+      if (lane == 0) {
+        if (boxes) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kSlots - 1) : "memory");
+        else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      }
+      __syncwarp();
       alignas(16) T v[kCols];
 #pragma unroll
       for (uint32_t c = 0; c < kCols; ++c)
@@ -230,21 +241,22 @@ __device__ __forceinline__ void store_rows(const GemmParams& p, const float (&ac
 #pragma unroll
       for (uint32_t q = 0; q < 4u; ++q)
         *reinterpret_cast<uint4*>(stage + lane * 64u + ((q ^ ((lane >> 1) & 3u)) << 4)) = reinterpret_cast<const uint4*>(v)[q];
-      __syncwarp();
-#pragma unroll
-      for (uint32_t i = 0; i < 4u; ++i) {
-        const uint32_t r = i * 8u + (lane >> 2), q = lane & 3u, c = c0 + q * kPer;
-        const uint4 w = *reinterpret_cast<const uint4*>(stage + r * 64u + ((q ^ ((r >> 1) & 3u)) << 4));
-        if (r < rows) {
-          T* to = out + (row0 + r) * p.g.out_stride + col0 + c;
-          if (p.wide_out && c + kPer <= cols) {
-            *reinterpret_cast<uint4*>(to) = w;
-          } else {
-            const T* parts = reinterpret_cast<const T*>(&w);
-            for (uint32_t e = 0; e < kPer; ++e)
-              if (c + e < cols) to[e] = parts[e];
-          }
+      if (boxes) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          tma_store_2d(&maps.out, smem_u32(stage), (int)(col0 + c0), (int)row0);
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
         }
+      } else {
+        // few rows, or rows that start anywhere: a lane a column, so that a warp stores what is contiguous (5789 x 4411 x 260: 181 us with
+        // a lane storing the 16 bytes it holds value by value)
+        __syncwarp();
+        const uint32_t c = c0 + lane % kCols, at = lane % kCols * sizeof(T);
+#pragma unroll 4
+        for (uint32_t r = lane / kCols; r < rows; r += 32u / kCols)
+          if (c < cols)
+            out[(row0 + r) * p.g.out_stride + col0 + c] = *reinterpret_cast<const T*>(stage + r * 64u + (((at >> 4) ^ ((r >> 1) & 3u)) << 4) + (at & 15u));
       }
       __syncwarp();
     }
@@ -254,6 +266,11 @@ __device__ __forceinline__ void store_rows(const GemmParams& p, const float (&ac
 template <int PAIR, int BN>
 constexpr uint32_t kGemmStageBytes = (kRowsCta + (uint32_t)BN / PAIR) * kBlockK;
 // Products of the scales of a row and of 128 columns, [2][BN / 128][kScaleBlocks][kScaleRow].
+// Output slots of a warp: a tile's columns in 16 bits.
+template <int BN>
+constexpr uint32_t kOutSlots = BN / 64;
+template <int BN>
+constexpr uint32_t kOutBytes = kSumWarps * kOutSlots<BN> * kSlotBytes;
 template <int BN>
 constexpr uint32_t kScaleBytes = 2u * (BN / 128) * kScaleBlocks * kScaleRow * 4u;
 
@@ -267,8 +284,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
   extern __shared__ uint8_t gemm_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)gemm_raw + 1023) & ~(uintptr_t)1023);
   uint8_t* out_stage = smem + p.stages * kStage;
-  float* scales = reinterpret_cast<float*>(out_stage + kSumWarps * kStageOutBytes);
-  GemmCtl* ctl = reinterpret_cast<GemmCtl*>(out_stage + kSumWarps * kStageOutBytes + kScaleBytes<BN>);
+  float* scales = reinterpret_cast<float*>(out_stage + kOutBytes<BN>);
+  GemmCtl* ctl = reinterpret_cast<GemmCtl*>(out_stage + kOutBytes<BN> + kScaleBytes<BN>);
   uint32_t* offsets = reinterpret_cast<uint32_t*>(ctl + 1);
   uint32_t* first = offsets + p.g.experts + 1u;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
@@ -362,7 +379,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
       // ------------------------------------------------------------ scales
       // Eight lanes read eight blocks of a row (a sector), and leave the products where a warp of the sums finds a block of
       // its 32 rows side by side.
-      constexpr uint32_t kHalves = BN / 128, kAtOnce = 8;
+      constexpr uint32_t kHalves = BN / 128, kAtOnce = BN == 128 ? 32 : 16;
       const uint32_t kb_off = lane & 7u, r_off = lane >> 3;
       uint32_t cb = 0, cph = 0;
       for (uint32_t t = t0; t < tiles && !failed; t += step) {
@@ -397,7 +414,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
     if (BN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     constexpr int NC = BN / 2;                 // columns of a warp
     const uint32_t quarter = warp & 3u, part = (warp - kFirstSumWarp) >> 2;
-    uint8_t* stage = out_stage + (warp - kFirstSumWarp) * kStageOutBytes;
+    uint8_t* slots = out_stage + (warp - kFirstSumWarp) * (kOutSlots<BN> * kSlotBytes);
     uint32_t s = 0, ph = 0, buf = 0, cb = 0, cph = 0;
     for (uint32_t t = t0; t < tiles && !failed; t += step) {
       float acc[NC];
@@ -447,10 +464,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
       const uint32_t rows = row0 < tile.row_end ? min(32u, tile.row_end - row0) : 0u;
       const uint32_t cols = col0 < p.g.n ? min((uint32_t)NC, p.g.n - col0) : 0u;
       const float* bias = p.g.bias ? p.g.bias + (uint64_t)tile.expert * p.g.n + col0 : nullptr;
-      if (p.g.out_dtype == PSB_DT_F32) store_rows<float, NC>(p, acc, stage, row0, rows, col0, cols, bias, lane);
-      else if (p.g.out_dtype == PSB_DT_BF16) store_rows<__nv_bfloat16, NC>(p, acc, stage, row0, rows, col0, cols, bias, lane);
-      else store_rows<__half, NC>(p, acc, stage, row0, rows, col0, cols, bias, lane);
+      if (p.g.out_dtype == PSB_DT_F32) store_rows<float, NC, kOutSlots<BN>>(maps, p, acc, slots, row0, rows, col0, cols, bias, lane);
+      else if (p.g.out_dtype == PSB_DT_BF16) store_rows<__nv_bfloat16, NC, kOutSlots<BN>>(maps, p, acc, slots, row0, rows, col0, cols, bias, lane);
+      else store_rows<__half, NC, kOutSlots<BN>>(maps, p, acc, slots, row0, rows, col0, cols, bias, lane);
     }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
 
   // ---------------------------------------------------------------- common exit
@@ -830,7 +848,16 @@ psb_status launch_tiles(psb_ctx* ctx, const Fp8GemmArgs& a, cudaStream_t s) {
   const psb_status st = fill_params(ctx, a, BN, kRowsCta, BN / PAIR, maps, p);
   if (st != PSB_OK) return st;
   p.idesc = instruction(a.a_dtype, a.b_dtype, kRowsCta * PAIR, BN);
-  const uint32_t rest = kSumWarps * kStageOutBytes + kScaleBytes<BN> + sizeof(GemmCtl) + runs_bytes(a) + 1024u;
+  if (p.wide_out) {
+    const bool wide = a.out_dtype == PSB_DT_F32;
+    cuuint64_t dims[2] = {a.n, a.rows}, strides[1] = {a.out_stride * (wide ? 4u : 2u)};
+    cuuint32_t box[2] = {wide ? 16u : 32u, 32u}, estr[2] = {1, 1};
+    if (((EncodeTiled)ctx->encode_tiled)(&maps.out, wide ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, a.out, dims, strides, box,
+                                         estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return PSB_ERR_CUDA;
+  }
+  const uint32_t rest = kOutBytes<BN> + kScaleBytes<BN> + sizeof(GemmCtl) + runs_bytes(a) + 1024u;
   p.stages = (uint32_t)((kSmemBudget - rest) / kGemmStageBytes<PAIR, BN>);
   if (p.stages > kMaxRing) p.stages = kMaxRing;
   const uint64_t tiles = row_tiles(a, kRowsCta * PAIR) * p.n_tiles;
