@@ -204,62 +204,112 @@ __device__ __forceinline__ void fma_pair(float& x, float& y, uint32_t u, uint32_
 }
 
 template <typename T> __device__ __forceinline__ T round_to(float v);
-template <> __device__ __forceinline__ float round_to<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 round_to<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half round_to<__half>(float v) { return __float2half_rn(v); }
 
+// NaN stays NaN.
+__device__ __forceinline__ float relu_of(float y) {
+  float r;
+  asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(y));
+  return r;
+}
 __device__ __forceinline__ float finish(float y, const float* bias, uint32_t relu) {
   if (bias) y += __ldca(bias);
-  return relu && y < 0.0f ? 0.0f : y;
+  return relu ? relu_of(y) : y;
+}
+__device__ __forceinline__ uint32_t pack_halves(float lo, float hi, bool bf16) {
+  uint32_t b, h;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b) : "f"(hi), "f"(lo));
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(hi), "f"(lo));
+  return bf16 ? b : h;
 }
 
-// A warp's 32 rows (a row a lane) of NC columns leave through shared memory, 64 bytes of a row at a time.  Whole boxes of 32 rows are
-// taken by the copy engine (its 64-byte swizzle is the order that keeps the lanes' 16-byte pieces in different banks), so that
-// the warp is back at its sums while they drain: all SMs store at the same time.  `rows`: rows of these 32 that exist; `cols`:
-// columns that exist from the first one on.
-template <typename T, int NC, uint32_t kSlots>
-__device__ __forceinline__ void store_rows(const GemmMaps& maps, const GemmParams& p, const float (&acc)[NC], uint8_t* slots, uint64_t row0,
-                                           uint32_t rows, uint32_t col0, uint32_t cols, const float* bias, uint32_t lane) {
-  constexpr uint32_t kCols = 64 / sizeof(T);
-  T* out = (T*)p.g.out;
-#pragma unroll
-  for (uint32_t c0 = 0; c0 < (uint32_t)NC; c0 += kCols) {
-    if (c0 < cols) {               // (the same for the whole warp)
-      // (the engine cuts a box at the end of a row to pieces of 16 bytes, not to elements)
-      const bool boxes = p.wide_out && rows == 32u && c0 + kCols <= cols;
-      uint8_t* stage = slots + (boxes ? c0 / kCols % kSlots * kSlotBytes : 0u);
-      // the slot's last box has been read
-      if (lane == 0) {
-        if (boxes) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kSlots - 1) : "memory");
-        else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-      }
-      __syncwarp();
-      alignas(16) T v[kCols];
-#pragma unroll
-      for (uint32_t c = 0; c < kCols; ++c)
-        v[c] = round_to<T>(finish(acc[c0 + c], bias && c0 + c < cols ? bias + c0 + c : nullptr, p.g.relu));
-#pragma unroll
-      for (uint32_t q = 0; q < 4u; ++q)
-        *reinterpret_cast<uint4*>(stage + lane * 64u + ((q ^ ((lane >> 1) & 3u)) << 4)) = reinterpret_cast<const uint4*>(v)[q];
-      if (boxes) {
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) {
-          tma_store_2d(&maps.out, smem_u32(stage), (int)(col0 + c0), (int)row0);
-          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        }
-      } else {
-        // few rows, or rows that start anywhere: a lane a column, so that a warp stores what is contiguous (5789 x 4411 x 260: 181 us with
-        // a lane storing the 16 bytes it holds value by value)
-        __syncwarp();
-        const uint32_t c = c0 + lane % kCols, at = lane % kCols * sizeof(T);
+// Slots of 32 rows x 64 bytes on their way to memory, columns of `size` bytes from c0 on.  Whole boxes are taken by the copy engine (its 64-byte
+// swizzle is the order that keeps the lanes' 16-byte pieces in different banks), so that the warp is back at its sums while
+// they drain: all SMs store at the same time.
+template <uint32_t kSlots>
+__device__ __forceinline__ void send_slots(const GemmMaps& maps, const GemmParams& p, uint8_t* slots, uint32_t size, uint64_t row0, uint32_t rows,
+                                           uint32_t col0, uint32_t c0, uint32_t cols, uint32_t lane) {
+  const uint32_t per = 64u / size;
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+#pragma unroll 1
+  for (uint32_t i = 0; i < kSlots; ++i, c0 += per) {
+    if (c0 >= cols) break;
+    const uint8_t* slot = slots + i * kSlotBytes;
+    // (the engine cuts a box at the end of a row to pieces of 16 bytes, not to elements)
+    if (p.wide_out && rows == 32u && c0 + per <= cols) {
+      if (lane == 0) tma_store_2d(&maps.out, smem_u32(slot), (int)(col0 + c0), (int)row0);
+    } else {
+      // a lane a column, so that a warp stores what is contiguous (5789 x 4411 x 260: 181 us with a lane storing the 16 bytes it
+      // holds value by value)
+      const uint32_t c = c0 + lane % per, at = lane % per * size;
+      if (c < cols) {
 #pragma unroll 4
-        for (uint32_t r = lane / kCols; r < rows; r += 32u / kCols)
-          if (c < cols)
-            out[(row0 + r) * p.g.out_stride + col0 + c] = *reinterpret_cast<const T*>(stage + r * 64u + (((at >> 4) ^ ((r >> 1) & 3u)) << 4) + (at & 15u));
+        for (uint32_t r = lane / per; r < rows; r += 32u / per) {
+          const uint8_t* from = slot + r * 64u + (((at >> 4) ^ ((r >> 1) & 3u)) << 4) + (at & 15u);
+          const uint64_t to = (row0 + r) * p.g.out_stride + col0 + c;
+          if (size == 4u) ((uint32_t*)p.g.out)[to] = *reinterpret_cast<const uint32_t*>(from);
+          else ((uint16_t*)p.g.out)[to] = *reinterpret_cast<const uint16_t*>(from);
+        }
       }
       __syncwarp();
     }
+  }
+  if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  __syncwarp();
+}
+
+__device__ __forceinline__ void put_row(uint8_t* slot, uint32_t lane, const uint32_t (&w)[16]) {
+#pragma unroll
+  for (uint32_t q = 0; q < 4u; ++q)
+    *reinterpret_cast<uint4*>(slot + lane * 64u + ((q ^ ((lane >> 1) & 3u)) << 4)) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+}
+
+// A warp's 32 rows (a row a lane) of NC columns: bias, ReLU, rounding, output.  `rows`: rows of these 32 that exist; `cols`: columns that
+// exist from the first one on.  The code is kept small: it is run once a tile, and the warps meet it cold (a copy of all of it for every
+// type and every 64 bytes of a row made 154 KB, and took 5400 clocks a tile).
+template <int NC, uint32_t kSlots>
+__device__ __forceinline__ void store_rows(const GemmMaps& maps, const GemmParams& p, float (&acc)[NC], uint8_t* slots, uint64_t row0, uint32_t rows,
+                                           uint32_t col0, uint32_t cols, const float* bias, uint32_t lane) {
+  if (bias) {
+    float mine[NC / 32];          // a lane's columns; the others' come from their lanes
+#pragma unroll
+    for (int i = 0; i < NC / 32; ++i) mine[i] = 32u * i + lane < cols ? __ldca(bias + 32u * i + lane) : 0.0f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] += __shfl_sync(0xFFFFFFFFu, mine[c / 32], c % 32);
+  }
+  if (p.g.relu) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] = relu_of(acc[c]);
+  }
+  if (p.g.out_dtype == PSB_DT_F32) {
+#pragma unroll
+    for (uint32_t c0 = 0; c0 < (uint32_t)NC; c0 += 16u * kSlots) {
+      if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the slots' last boxes have been read
+      __syncwarp();
+#pragma unroll
+      for (uint32_t i = 0; i < kSlots; ++i) {
+        uint32_t w[16];
+#pragma unroll
+        for (uint32_t c = 0; c < 16u; ++c) w[c] = __float_as_uint(acc[c0 + 16u * i + c]);
+        put_row(slots + i * kSlotBytes, lane, w);
+      }
+      send_slots<kSlots>(maps, p, slots, 4u, row0, rows, col0, c0, cols, lane);
+    }
+  } else {
+    static_assert(NC == 32 * kSlots, "a tile's columns in 16 bits fill the slots");
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+    const bool bf16 = p.g.out_dtype == PSB_DT_BF16;
+#pragma unroll
+    for (uint32_t i = 0; i < kSlots; ++i) {
+      uint32_t w[16];
+#pragma unroll
+      for (uint32_t c = 0; c < 16u; ++c) w[c] = pack_halves(acc[32u * i + 2u * c], acc[32u * i + 2u * c + 1u], bf16);
+      put_row(slots + i * kSlotBytes, lane, w);
+    }
+    send_slots<kSlots>(maps, p, slots, 2u, row0, rows, col0, 0u, cols, lane);
   }
 }
 
@@ -333,8 +383,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
       // (a copy instruction holds its thread for a few hundred clocks)
       if (lane == 0) {
         uint32_t s = 0, ph = 0;
+#pragma unroll 1
         for (uint32_t t = t0; t < tiles && !failed; t += step) {
           const GemmTile tile = tile_at<TM, BN>(p, t, first, offsets);
+#pragma unroll 1
           for (uint32_t kb = 0; kb < p.k_blocks; ++kb) {
             const uint32_t bar = PAIR == 2 ? in_cta(smem_u32(&ctl->full[s]), 0u) : smem_u32(&ctl->full[s]);
             const uint32_t dst = smem_u32(smem) + s * kStage;
@@ -355,7 +407,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
       if (rank == 0u) {
         uint32_t s = 0, ph = 0, buf = 0, bph = 0;
         const uint32_t desc_hi = smem_desc_hi(kBlockK);
+#pragma unroll 1
         for (uint32_t t = t0; t < tiles && !failed; t += step) {
+#pragma unroll 1
           for (uint32_t kb = 0; kb < p.k_blocks; ++kb) {
             if (!wait_warp(smem_u32(&ctl->full[s]), ph, p.polls) || !wait_warp(smem_u32(&ctl->acc_empty[buf]), bph ^ 1u, p.polls)) {
               failed = true;
@@ -382,11 +436,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
       constexpr uint32_t kHalves = BN / 128, kAtOnce = BN == 128 ? 32 : 16;
       const uint32_t kb_off = lane & 7u, r_off = lane >> 3;
       uint32_t cb = 0, cph = 0;
+#pragma unroll 1
       for (uint32_t t = t0; t < tiles && !failed; t += step) {
         const GemmTile tile = tile_at<TM, BN>(p, t, first, offsets);
         const uint32_t row = tile.row + rank * kRowsCta + r_off, last = min(tile.row_end, p.g.m) - 1u;
         const float* sb = p.g.b_scale + tile.expert * p.g.b_scale_expert_stride + (uint64_t)(tile.n0 / 128u) * p.g.b_scale_stride;
         const bool second = kHalves == 2u && tile.n0 + 128u < p.g.n;
+#pragma unroll 1
         for (uint32_t k0 = 0; k0 < p.k_blocks; k0 += kScaleBlocks) {
           const uint32_t kb = min(k0 + kb_off, p.k_blocks - 1u);
           const float b0 = __ldcg(sb + kb), b1 = second ? __ldcg(sb + p.g.b_scale_stride + kb) : 0.0f;
@@ -416,12 +472,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
     const uint32_t quarter = warp & 3u, part = (warp - kFirstSumWarp) >> 2;
     uint8_t* slots = out_stage + (warp - kFirstSumWarp) * (kOutSlots<BN> * kSlotBytes);
     uint32_t s = 0, ph = 0, buf = 0, cb = 0, cph = 0;
+#pragma unroll 1
     for (uint32_t t = t0; t < tiles && !failed; t += step) {
       float acc[NC];
 #pragma unroll
       for (int i = 0; i < NC; ++i) acc[i] = 0.0f;
       const uint32_t taddr = tmem_base + part * NC + ((quarter * 32u) << 16);
       const float* sc_of = scales + (part * NC / 128u) * kScaleBlocks * kScaleRow + quarter * 32u + lane;
+#pragma unroll 1
       for (uint32_t kb = 0; kb < p.k_blocks; ++kb) {
         if (kb % kScaleBlocks == 0u && !wait_warp(smem_u32(&ctl->scale_full[cb]), cph, p.polls)) { failed = true; break; }
         const float sc = sc_of[(cb * (BN / 128) * kScaleBlocks + kb % kScaleBlocks) * kScaleRow];
@@ -464,9 +522,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
       const uint32_t rows = row0 < tile.row_end ? min(32u, tile.row_end - row0) : 0u;
       const uint32_t cols = col0 < p.g.n ? min((uint32_t)NC, p.g.n - col0) : 0u;
       const float* bias = p.g.bias ? p.g.bias + (uint64_t)tile.expert * p.g.n + col0 : nullptr;
-      if (p.g.out_dtype == PSB_DT_F32) store_rows<float, NC, kOutSlots<BN>>(maps, p, acc, slots, row0, rows, col0, cols, bias, lane);
-      else if (p.g.out_dtype == PSB_DT_BF16) store_rows<__nv_bfloat16, NC, kOutSlots<BN>>(maps, p, acc, slots, row0, rows, col0, cols, bias, lane);
-      else store_rows<__half, NC, kOutSlots<BN>>(maps, p, acc, slots, row0, rows, col0, cols, bias, lane);
+      store_rows<NC, kOutSlots<BN>>(maps, p, acc, slots, row0, rows, col0, cols, bias, lane);
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
@@ -571,8 +627,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) stream_fp8_kernel(const __gri
     // -------------------------------------------------------------- copies: of the filter (warp 0), of a (warp 2)
     if (lane == 0) {
       uint32_t s = 0, ph = 0;
+#pragma unroll 1
       for (uint32_t t = t0; t < tiles && !failed; t += step) {
         const GemmTile tile = tile_at<BT, BN>(p, t, first, offsets);
+#pragma unroll 1
         for (uint32_t kb = k_lo; kb < k_hi; ++kb) {
           const uint32_t bar = smem_u32(&ctl->full[s]), dst = smem_u32(smem) + s * kStage;
           if (!wait_asleep<20>(smem_u32(&ctl->done[s]), ph ^ 1u, p.polls)) { failed = true; break; }
@@ -591,7 +649,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) stream_fp8_kernel(const __gri
     // -------------------------------------------------------------- MMA
     uint32_t s = 0, ph = 0, buf = 0, bph = 0;
     const uint32_t desc_hi = smem_desc_hi(kBlockK);
+#pragma unroll 1
     for (uint32_t t = t0; t < tiles && !failed; t += step) {
+#pragma unroll 1
       for (uint32_t kb = k_lo; kb < k_hi; ++kb) {
         if (!wait_warp(smem_u32(&ctl->full[s]), ph, p.polls) || !wait_warp(smem_u32(&ctl->acc_empty[buf]), bph ^ 1u, p.polls)) {
           failed = true;
@@ -614,10 +674,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1) stream_fp8_kernel(const __gri
     // -------------------------------------------------------------- scales: products for the rows of a, eight blocks at a time
     const uint32_t kb_off = lane & 7u, r_off = lane >> 3;
     uint32_t cb = 0, cph = 0;
+#pragma unroll 1
     for (uint32_t t = t0; t < tiles && !failed; t += step) {
       const GemmTile tile = tile_at<BT, BN>(p, t, first, offsets);
       const uint32_t row = tile.row + r_off, last = min(tile.row_end, p.g.m) - 1u;
       const float* sb = p.g.b_scale + tile.expert * p.g.b_scale_expert_stride + (uint64_t)(tile.n0 / 128u) * p.g.b_scale_stride;
+#pragma unroll 1
       for (uint32_t k0 = k_lo; k0 < k_hi; k0 += kScaleBlocks) {
         const uint32_t kb = min(k0 + kb_off, k_hi - 1u);
         const float b0 = __ldcg(sb + kb);
@@ -637,12 +699,15 @@ __global__ void __launch_bounds__(kGemmThreads, 1) stream_fp8_kernel(const __gri
     // -------------------------------------------------------------- scaled sums: a lane a column of out, a register a row
     const uint32_t quarter = warp & 3u, group = (warp - kFirstSumWarp) >> 2, col = quarter * 32u + lane;
     uint32_t s = 0, ph = 0, buf = 0, cb = 0, cph = 0, turn = 0;
+#pragma unroll 1
     for (uint32_t t = t0; t < tiles && !failed; t += step) {
       float acc[BT];
 #pragma unroll
       for (int i = 0; i < BT; ++i) acc[i] = 0.0f;
+#pragma unroll 1
       for (uint32_t k0 = k_lo; k0 < k_hi && !failed; k0 += kScaleBlocks) {
         if (!wait_warp(smem_u32(&ctl->scale_full[cb]), cph, p.polls)) { failed = true; break; }
+#pragma unroll 1
         for (uint32_t kb = k0; kb < min(k0 + kScaleBlocks, k_hi); ++kb) {
           if ((turn++ & 1u) == group) {
             if (!wait_warp(smem_u32(&ctl->done[s]), ph, p.polls)) { failed = true; break; }
