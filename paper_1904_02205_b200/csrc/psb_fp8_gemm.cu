@@ -3,8 +3,20 @@
 //   y[m][n] = sum_b sa[m][b] sb[n / 128][b] S_b[m][n],   S_b[m][n] = sum_{k in block b} a[m][k] b[n][k]
 //
 // The scales are arbitrary fp32 numbers, so the tensor cores can add up one block of 128 only; S_b goes from tensor
-// memory to registers, where the running sum is kept in fp32: one fma per output and block.  That is 1/128 of the MMA's
-// multiply-adds, on pipes that do 1/64 of its rate, so the epilogue warps keep up as long as they do little else.
+// memory to registers, where the running sum is kept in fp32: one fma per output and block, 1/128 of the MMA's
+// multiply-adds on pipes of 1/64 of its rate.
+//
+// Many rows (gemm_fp8_kernel): one persistent CTA an SM, or a pair of SMs on one tile (cta_group::2).  Warps of their own copy a, copy
+// b, issue the MMAs and multiply the scales; eight warps add up a block of 128 or 256 columns out of one TMEM buffer while the
+// MMAs of the next block fill the other, and hand finished tiles to the copy engine.  8192^3: 552 us cool, 590 to 670 in a
+// stream of calls under the power cap (2.0 to 1.64 PFLOP/s; clocks 1.65 GHz).  A block of 256 x 256 x 128 takes about 1000 clocks,
+// 512 of them the MMAs'.  Without the fmas, the output and three of four MMAs it takes 650: the wait for the MMAs, the
+// loads from TMEM and the hand-over follow one another, and two buffers are all that TMEM holds.  Measured and dropped: sixteen summing
+// warps (as fast), halves of the columns handed over one by one (604 us against 576), two warps that issue MMAs (no change),
+// 128 x 256 on single SMs (600), polls that read a clock, more code anywhere in the summing warps (154 KB of it cost 5400
+// clocks a tile).
+// Few rows (stream_fp8_kernel): the other way round, see there.
+
 #include "psb_mma.cuh"
 
 #include <cuda_bf16.h>
@@ -49,7 +61,7 @@ struct GemmCtl {
 };
 
 // Waits.  Their bound is counted in polls, without a clock: what reads the clock and the give-up flag of the CTA costs registers
-// and code beside 128 accumulators (8192^3: 541 us like this, 585 with it, 635 where it spilled).  A poll takes from 20 clocks
+// and code beside 128 accumulators (8192^3 at the time: 541 us like this, 585 with it, 635 where it spilled).  A poll takes from 20 clocks
 // to the microseconds for which the hardware suspends it.  A whole warp leaves its wait in one piece, as the tcgen05
 // instructions behind it want; a warp that is ahead of the others sleeps between polls and leaves them the issue slots.
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint32_t polls) {
@@ -194,7 +206,7 @@ __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint32_t a_lo, uint32_t 
         ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(desc_hi), "r"(idesc), "r"(acc));
 }
 
-// Two sums at once, each as fmaf: half of the instructions.
+// Two sums at once, each as fmaf (8192^3 551 us, 565 one by one).
 __device__ __forceinline__ void fma_pair(float& x, float& y, uint32_t u, uint32_t v, float s) {
   asm("{\n\t.reg .b64 a, b, c;\n\t"
       "mov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %3};\n\tmov.b64 c, {%4, %4};\n\t"
@@ -315,12 +327,12 @@ __device__ __forceinline__ void store_rows(const GemmMaps& maps, const GemmParam
 
 template <int PAIR, int BN>
 constexpr uint32_t kGemmStageBytes = (kRowsCta + (uint32_t)BN / PAIR) * kBlockK;
-// Products of the scales of a row and of 128 columns, [2][BN / 128][kScaleBlocks][kScaleRow].
-// Output slots of a warp: a tile's columns in 16 bits.
+// Output slots of a warp: its columns of a tile in 16 bits.
 template <int BN>
 constexpr uint32_t kOutSlots = BN / 64;
 template <int BN>
 constexpr uint32_t kOutBytes = kSumWarps * kOutSlots<BN> * kSlotBytes;
+// Products of the scales of a row and of 128 columns, [2][BN / 128][kScaleBlocks][kScaleRow].
 template <int BN>
 constexpr uint32_t kScaleBytes = 2u * (BN / 128) * kScaleBlocks * kScaleRow * 4u;
 
@@ -984,18 +996,22 @@ psb_status launch_gemm_fp8(psb_ctx* ctx, const Fp8GemmArgs& given, void* scratch
   }
   // Few rows (on average, where they are dealt out to experts) stream the filter; us, streamed with 16 / 32 / 64 rows a tile against
   // tiles of 128 x 128: 4096 x 4096 with 17 rows 10.6 / 10.5 / 11.3 / 17.4, 64 rows 13.7 / 11.4 / 11.1 / 17.7, 128 rows 22.9 / 16.9 /
-  // 17.2 / 17.1, 512 rows 67.8 / 47.1 / 30.5 / 17.9; 64 experts of 2048 x 2048 with 4 rows each 44.1 / 46.5 / 52.4 / 64.7, with 16 rows
-  // 66.4 / 58.1 / 60.5 / 70.6, with 64 rows 178 / 129 / 106 / 89.
+  // 15.6 / 16.6, 192 rows - / 26.5 / 18.1 / 15.8; 64 experts of 2048 x 2048 with 4 rows each 44.1 / 46.5 / 52.4 / 64.7, with 16 rows
+  // 66.4 / 58.1 / 60.5 / 70.6, with 32 rows - / 77 / 72 / 65.
   const uint32_t each = a.experts ? (a.rows + a.experts - 1u) / a.experts : a.m;
   if (each <= (a.experts ? 8u : 16u)) return launch_stream<16>(ctx, a, s);
-  if (each <= 32u) return launch_stream<32>(ctx, a, s);
+  if (each <= (a.experts ? 24u : 32u)) return launch_stream<32>(ctx, a, s);
   if (!a.experts && each <= 128u) return launch_stream<64>(ctx, a, s);
-  // Tiles of 256 x 256 by pairs of SMs move two thirds of the bytes of single SMs' 128 x 128 per product, and take 640 ns a
-  // block for four times their 390; what counts is the number of rounds of tiles.  8192^3 580 us against 692, 4096^3 99.7 and 99.5,
-  // 1500 x 1000 x 2048 19.4 and 12.8, 512 x 4096 x 4096 27.7 and 17.9, 16384 rows over 8 experts of 4096 x 4096 377 and 397.
-  const uint64_t of_experts = a.experts ? a.experts : 1u, sms = (uint64_t)ctx->sm_count;
-  const uint64_t pairs = of_experts * ((each + 255u) / 256u) * ((a.n + 255u) / 256u), singles = of_experts * ((each + 127u) / 128u) * ((a.n + 127u) / 128u);
-  if ((pairs + sms / 2u - 1u) / (sms / 2u) * 64u < (singles + sms - 1u) / sms * 39u) return launch_tiles<2, 256>(ctx, a, s);
+  // Tiles of 256 x 256 by pairs of SMs read half of the bytes per product that single SMs' 128 x 128 do, and take 1.8 times as long a
+  // block for twice an SM's work; what counts is the number of rounds of tiles (in halves: a run of an expert ends in the middle of a
+  // tile).  us, pairs against singles: 8192^3 599 and 667, 4096^3 97 and 95, 1500 x 1000 x 2048 20.6 and 12.7, 3000 x 2500 x 1000
+  // 29.5 and 30.6, 512 x 4096 x 4096 28 and 18; 16384 rows over 8 experts of 4096 x 4096 321 and 361, over 64 of 2048 x 2048 179 and 151.
+  const uint64_t sms = (uint64_t)ctx->sm_count, of = a.experts ? a.experts : 1u;
+  auto rounds = [&](uint32_t tile, uint64_t at_once) {
+    const uint64_t halves = a.experts ? 2u * each / tile + 1u : 2u * ((each + tile - 1u) / tile);
+    return (of * halves * ((a.n + tile - 1u) / tile) + 2u * at_once - 1u) / (2u * at_once);
+  };
+  if (rounds(256, sms / 2u) * 9u < rounds(128, sms) * 5u) return launch_tiles<2, 256>(ctx, a, s);
   return launch_tiles<1, 128>(ctx, a, s);
 }
 
