@@ -8,13 +8,13 @@
 //
 // Many rows (gemm_fp8_kernel): one persistent CTA an SM, or a pair of SMs on one tile (cta_group::2).  Warps of their own copy a, copy
 // b, issue the MMAs and multiply the scales; eight warps add up a block of 128 or 256 columns out of one TMEM buffer while the
-// MMAs of the next block fill the other, and hand finished tiles to the copy engine.  8192^3: 552 us cool, 590 to 670 in a
-// stream of calls under the power cap (2.0 to 1.64 PFLOP/s; clocks 1.65 GHz).  A block of 256 x 256 x 128 takes about 1000 clocks,
-// 512 of them the MMAs'.  Without the fmas, the output and three of four MMAs it takes 650: the wait for the MMAs, the
-// loads from TMEM and the hand-over follow one another, and two buffers are all that TMEM holds.  Measured and dropped: sixteen summing
-// warps (as fast), halves of the columns handed over one by one (604 us against 576), two warps that issue MMAs (no change),
-// 128 x 256 on single SMs (600), polls that read a clock, more code anywhere in the summing warps (154 KB of it cost 5400
-// clocks a tile).
+// MMAs of the next block fill the other, and hand finished tiles to the copy engine.  8192^3: 500 us (2.2 PFLOP/s; the clocks sink
+// to 1.65 GHz under the power cap in a long stream of calls).  A block of 256 x 256 x 128 takes about 950 clocks, 512 of them the
+// MMAs'; in an earlier state, with one of four MMAs and neither fmas nor output, it took 650: the wait for the MMAs, the loads from TMEM
+// and the hand-over follow one another, and two buffers are all that TMEM holds.  Measured and dropped: sixteen summing warps
+// (as fast), halves of the columns handed over one by one (604 us against 576), two warps that issue MMAs (no change), 128 x 256 on
+// single SMs (600), a block's first columns fetched before the last arithmetic of the block before it (575 against 560), polls
+// that read a clock, more code anywhere in the summing warps (154 KB of it cost 5400 clocks a tile).
 // Few rows (stream_fp8_kernel): the other way round, see there.
 
 #include "psb_mma.cuh"
@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
   bool failed = false;
 
   if (warp < kFirstSumWarp) {
-    if (BN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (BN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == 0 || warp == 2) {
       // ------------------------------------------------------------ copies: of a, and of b by a warp of their own
       // (a copy instruction holds its thread for a few hundred clocks)
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
     }
   } else {
     // -------------------------------------------------------------- scaled sums and output
-    if (BN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    if (BN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     constexpr int NC = BN / 2;                 // columns of a warp
     const uint32_t quarter = warp & 3u, part = (warp - kFirstSumWarp) >> 2;
     uint8_t* slots = out_stage + (warp - kFirstSumWarp) * (kOutSlots<BN> * kSlotBytes);
@@ -508,15 +508,15 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
           }
           __syncwarp();
         };
-        uint32_t v[2][16];
-        tc_ld16(taddr + buf * BN, v[0]);
+        // (one load at a time: the other warp of the scheduler computes meanwhile; a second one in flight took 8192^3 from 505 us to 560)
 #pragma unroll
         for (int c = 0; c < NC / 16; ++c) {
+          uint32_t v[16];
+          tc_ld16(taddr + buf * BN + c * 16, v);
           tc_wait_ld();
           if (c + 1 == NC / 16) handed_back();
-          else tc_ld16(taddr + buf * BN + (c + 1) * 16, v[(c + 1) & 1]);
 #pragma unroll
-          for (int i = 0; i < 16; i += 2) fma_pair(acc[c * 16 + i], acc[c * 16 + i + 1], v[c & 1][i], v[c & 1][i + 1], sc);
+          for (int i = 0; i < 16; i += 2) fma_pair(acc[c * 16 + i], acc[c * 16 + i + 1], v[i], v[i + 1], sc);
         }
         if (++s == p.stages) { s = 0; ph ^= 1u; }
         if (++buf == kBufs) buf = 0;
@@ -1002,16 +1002,17 @@ psb_status launch_gemm_fp8(psb_ctx* ctx, const Fp8GemmArgs& given, void* scratch
   if (each <= (a.experts ? 8u : 16u)) return launch_stream<16>(ctx, a, s);
   if (each <= (a.experts ? 24u : 32u)) return launch_stream<32>(ctx, a, s);
   if (!a.experts && each <= 128u) return launch_stream<64>(ctx, a, s);
-  // Tiles of 256 x 256 by pairs of SMs read half of the bytes per product that single SMs' 128 x 128 do, and take 1.8 times as long a
+  // Tiles of 256 x 256 by pairs of SMs read half of the bytes per product that single SMs' 128 x 128 do, and take 1.65 times as long a
   // block for twice an SM's work; what counts is the number of rounds of tiles (in halves: a run of an expert ends in the middle of a
-  // tile).  us, pairs against singles: 8192^3 599 and 667, 4096^3 97 and 95, 1500 x 1000 x 2048 20.6 and 12.7, 3000 x 2500 x 1000
-  // 29.5 and 30.6, 512 x 4096 x 4096 28 and 18; 16384 rows over 8 experts of 4096 x 4096 321 and 361, over 64 of 2048 x 2048 179 and 151.
+  // tile).  us, pairs against singles: 8192^3 523 and 622, 4096^3 90 and 96, 1500 x 1000 x 2048 18.6 and 12.3, 3000 x 2500 x 1000
+  // 27.4 and 32.3, 512 x 4096 x 4096 24.6 and 17.6; 16384 rows over 8 experts of 4096 x 4096 300 and 340, over 64 of 2048 x 2048 163 and 147,
+  // 1884 over 18 of 2048 x 3344 68 and 50.
   const uint64_t sms = (uint64_t)ctx->sm_count, of = a.experts ? a.experts : 1u;
   auto rounds = [&](uint32_t tile, uint64_t at_once) {
-    const uint64_t halves = a.experts ? 2u * each / tile + 1u : 2u * ((each + tile - 1u) / tile);
+    const uint64_t part = 2u * (uint64_t)each / tile + 1u, halves = !a.experts ? 2u * ((each + tile - 1u) / tile) : part < 2u ? 2u : part;
     return (of * halves * ((a.n + tile - 1u) / tile) + 2u * at_once - 1u) / (2u * at_once);
   };
-  if (rounds(256, sms / 2u) * 9u < rounds(128, sms) * 5u) return launch_tiles<2, 256>(ctx, a, s);
+  if (rounds(256, sms / 2u) * 33u < rounds(128, sms) * 20u) return launch_tiles<2, 256>(ctx, a, s);
   return launch_tiles<1, 128>(ctx, a, s);
 }
 
