@@ -6,8 +6,8 @@
 // they are further apart than their error bound (kRound), and the row is done again in 64 bits where they are not (equal
 // logits with equal biases are equal, and need no second look).
 // The order of the choices is a counting sort: blocks of consecutive rows count their choices per expert, a second launch
-// sums the counts of the blocks before each, a third places the choices, the rank inside a block being the number of
-// earlier rows that chose the same expert (bit masks over the block's rows).  Nothing depends on the order of atomics.
+// adds up the counts of the blocks before each (from 37741 rows on a launch between them does) and places the choices, the rank inside
+// a block being the number of earlier rows that chose the same expert (bit masks over the block's rows).  Nothing depends on the order of atomics.
 // Up to 64 rows one block does all three.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -41,8 +41,11 @@ struct RouteArgs {
   uint32_t block_rows, blocks;
   uint32_t alone;            // one block has all rows and places them itself
   uint32_t wide;             // rows of logits start at multiples of 16 bytes
+  uint32_t groups_of_counts; // counts are bytes, and so many threads add up the counts of four experts; 0: words, added up by scan_kernel
   uint32_t lanes_per_group;  // a power of two where groups are the experts of whole lanes, else 0
 };
+
+__host__ __device__ __forceinline__ uint32_t round_up4(uint32_t n) { return (n + 3u) & ~3u; }
 
 // Monotone map of fp32 numbers onto words, kNone below all of them; and of fp64 numbers, 0 below all of them.
 constexpr int kNone = (int)0x80000000;
@@ -402,18 +405,25 @@ __device__ __forceinline__ void route_row(const RouteArgs& a, uint32_t t, const 
   w = mine ? s * a.scaling : 0.0f;
 }
 
-// Places of the choices of rows [lo, hi).  Shared memory: place [experts], the first place of each expert for these rows, and
-// bits [experts][words], zeros, a bit for each of the rows.
-__device__ __forceinline__ void place_choices(const RouteArgs& a, uint32_t lo, uint32_t hi, const uint32_t* place, uint32_t* bits, uint32_t words) {
+// The choices of rows [lo, hi) are placed in two steps, so that other work may lie between them.  Shared memory: bits
+// [experts][words], zeros at first, a bit for each of the rows; place [experts], the first place of each expert for these rows.
+// `id`: the thread's first choice.
+__device__ __forceinline__ int first_choice(const RouteArgs& a, uint32_t lo, uint32_t hi) {
+  return threadIdx.x < (hi - lo) * a.top_k ? __ldcg(a.ids + (size_t)lo * a.top_k + threadIdx.x) : -1;
+}
+__device__ __forceinline__ void mark_choices(const RouteArgs& a, uint32_t lo, uint32_t hi, int id, uint32_t* bits, uint32_t words) {
   const uint32_t choices = (hi - lo) * a.top_k;
   for (uint32_t i = threadIdx.x; i < choices; i += blockDim.x) {
-    const int id = __ldcg(a.ids + (size_t)lo * a.top_k + i);
+    if (i != threadIdx.x) id = __ldcg(a.ids + (size_t)lo * a.top_k + i);
     const uint32_t r = i / a.top_k;
     if (id >= 0) atomicOr(&bits[(uint32_t)id * words + r / 32u], 1u << (r & 31u));
   }
-  __syncthreads();
+}
+__device__ __forceinline__ void place_choices(const RouteArgs& a, uint32_t lo, uint32_t hi, int id, const uint32_t* place, const uint32_t* bits,
+                                              uint32_t words) {
+  const uint32_t choices = (hi - lo) * a.top_k;
   for (uint32_t i = threadIdx.x; i < choices; i += blockDim.x) {
-    const int id = __ldcg(a.ids + (size_t)lo * a.top_k + i);
+    if (i != threadIdx.x) id = __ldcg(a.ids + (size_t)lo * a.top_k + i);
     const uint32_t r = i / a.top_k;
     int at = -1;
     if (id >= 0) {
@@ -484,7 +494,10 @@ __global__ void __launch_bounds__(kRouteThreads<EL>) route_kernel(const RouteArg
   if (!a.order) return;
   __syncthreads();
   if (!a.alone) {
-    for (uint32_t e = threadIdx.x; e < a.experts; e += blockDim.x) a.counts[(size_t)blockIdx.x * a.experts + e] = hist[e];
+    for (uint32_t e = threadIdx.x; e < a.experts; e += blockDim.x) {
+      if (a.groups_of_counts) ((uint8_t*)a.counts)[(size_t)blockIdx.x * round_up4(a.experts) + e] = (uint8_t)hist[e];
+      else a.counts[(size_t)blockIdx.x * a.experts + e] = hist[e];
+    }
     return;
   }
   uint32_t carry = 0;
@@ -500,13 +513,16 @@ __global__ void __launch_bounds__(kRouteThreads<EL>) route_kernel(const RouteArg
   }
   if (threadIdx.x == 0u) a.offsets[a.experts] = (int32_t)carry;
   __syncthreads();
-  place_choices(a, lo, hi, hist, hist + a.experts, words);
+  const int id = first_choice(a, lo, hi);
+  mark_choices(a, lo, hi, id, hist + a.experts, words);
+  __syncthreads();
+  place_choices(a, lo, hi, id, hist, hist + a.experts, words);
   for (uint32_t i = carry + threadIdx.x; i < a.tokens * a.top_k; i += blockDim.x) a.order[i] = -1;
 }
 
 // Turns the counts of the blocks into the numbers of rows before each block, expert by expert, and adds the sums as one row more.
-// 32 experts a block of threads, the counting blocks dealt out to 32 threads each.  (Every placing block adding up all
-// counts took 12 us of 148 SMs on the same 150 KB.)
+// 32 experts a block of threads, the counting blocks dealt out to 32 threads each.  (Where counts are words: every placing block adding
+// them up took 12 us, 148 SMs on the same 150 KB.)
 __global__ void __launch_bounds__(1024) scan_kernel(const RouteArgs a) {
   pdl_prologue();
   __shared__ uint32_t sums[32][33];
@@ -532,7 +548,8 @@ __global__ void __launch_bounds__(1024) scan_kernel(const RouteArgs a) {
   if (y == 31u) a.counts[(size_t)a.blocks * a.experts + e] = before;
 }
 
-// Places the choices of each block.  Dynamic shared memory: places [experts], the bits of place_choices.
+// Places the choices of each block.  Dynamic shared memory: places [experts], the bits of place_choices, sums of bytes
+// [groups_of_counts][2][experts].
 __global__ void __launch_bounds__(1024) order_kernel(const RouteArgs a) {
   pdl_prologue();
   extern __shared__ uint32_t order_smem[];
@@ -540,9 +557,45 @@ __global__ void __launch_bounds__(1024) order_kernel(const RouteArgs a) {
   const uint32_t words = (a.block_rows + 31u) / 32u;
   uint32_t *place = order_smem, *bits = place + a.experts;
   const uint32_t lo = blockIdx.x * a.block_rows, hi = min(lo + a.block_rows, a.tokens), e = threadIdx.x;
-  const uint32_t all = e < a.experts ? __ldcg(a.counts + (size_t)a.blocks * a.experts + e) : 0u;
-  const uint32_t earlier = e < a.experts ? __ldcg(a.counts + (size_t)blockIdx.x * a.experts + e) : 0u;
+  const int id = first_choice(a, lo, hi);
   for (uint32_t i = threadIdx.x; i < a.experts * words; i += blockDim.x) bits[i] = 0u;
+  uint32_t all = 0u, earlier = 0u;
+  if (a.groups_of_counts) {
+    // four experts in a word, added up in 16 bits: 148 blocks of at most 255 rows
+    const uint32_t quads = round_up4(a.experts) / 4u, q = threadIdx.x % quads, g = threadIdx.x / quads;
+    uint32_t* sums = bits + a.experts * words;
+    if (g < a.groups_of_counts) {
+      const uint32_t b_lo = a.blocks * g / a.groups_of_counts, b_hi = a.blocks * (g + 1u) / a.groups_of_counts;
+      uint32_t sum[2] = {0u, 0u}, before[2] = {0u, 0u};
+#pragma unroll 10
+      for (uint32_t b = b_lo; b < b_hi; ++b) {
+        const uint32_t w = __ldcg(a.counts + (size_t)b * quads + q);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t pair = (w >> (8 * h)) & 0x00FF00FFu;
+          sum[h] += pair;
+          before[h] += b < blockIdx.x ? pair : 0u;
+        }
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < 4u; ++k) {
+        sums[(2u * g) * quads * 4u + 4u * q + k] = (sum[k & 1u] >> (16u * (k >> 1))) & 0xFFFFu;
+        sums[(2u * g + 1u) * quads * 4u + 4u * q + k] = (before[k & 1u] >> (16u * (k >> 1))) & 0xFFFFu;
+      }
+    }
+    __syncthreads();
+    if (e < a.experts) {
+      for (uint32_t k = 0; k < a.groups_of_counts; ++k) {
+        all += sums[2u * k * quads * 4u + e];
+        earlier += sums[(2u * k + 1u) * quads * 4u + e];
+      }
+    }
+  } else if (e < a.experts) {
+    all = __ldcg(a.counts + (size_t)a.blocks * a.experts + e);
+    earlier = __ldcg(a.counts + (size_t)blockIdx.x * a.experts + e);
+  }
+  __syncthreads();
+  mark_choices(a, lo, hi, id, bits, words);
   uint32_t used;
   const uint32_t start = sum_before(all, warp_total, used);      // (at most 1024 experts: a thread each)
   if (e < a.experts) {
@@ -551,16 +604,17 @@ __global__ void __launch_bounds__(1024) order_kernel(const RouteArgs a) {
   }
   if (blockIdx.x == 0u && threadIdx.x == 0u) a.offsets[a.experts] = (int32_t)used;
   __syncthreads();
-  place_choices(a, lo, hi, place, bits, words);
+  place_choices(a, lo, hi, id, place, bits, words);
   // behind the last
   const uint64_t end = (uint64_t)a.tokens * a.top_k;
   for (uint64_t i = used + (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < end; i += (uint64_t)gridDim.x * blockDim.x) a.order[i] = -1;
 }
 
 uint32_t rows_of_a_block(const psb_route_desc& d) {
-  // a block per SM; up to 64 rows one block alone, which spares two launches (4 us of the host's time)
+  // a block per SM; up to 64 rows one block alone, which spares a launch or two
+  if (d.tokens <= 64u) return 64u;
   const uint32_t rows = (d.tokens + kSms - 1u) / kSms;
-  return rows < 64u ? 64u : rows < kMaxBlockRows ? rows : kMaxBlockRows;
+  return rows < 8u ? 8u : rows < kMaxBlockRows ? rows : kMaxBlockRows;
 }
 
 // ---- combine -------------------------------------------------------------------------------------------------------------
@@ -709,6 +763,10 @@ cudaError_t launch_route(const void* logits, const float* bias, const uint8_t* m
   a.blocks = (d.tokens + a.block_rows - 1u) / a.block_rows;
   a.alone = a.blocks == 1u;
   a.wide = (((uintptr_t)logits | d.logit_stride * (d.in_dtype == PSB_DT_F32 ? 4u : 2u)) & 15u) == 0u;
+  // a block's counts in bytes: every placing block adds up those of all 148 itself (16384 rows over 256 experts 27.3 us, 28.2 with scan_kernel
+  // between, and a launch less for the host)
+  const uint32_t quads = round_up4(d.experts) / 4u;
+  a.groups_of_counts = a.block_rows > 255u || a.blocks > kSms ? 0u : 1024u / quads < 16u ? 1024u / quads : 16u;
   uint32_t el = 1;
   while (el * 32u < d.experts) el *= 2u;
   const uint32_t size = d.experts / d.groups, lanes = size / el;
@@ -727,9 +785,11 @@ cudaError_t launch_route(const void* logits, const float* bias, const uint8_t* m
   else go(route_kernel<32>, kRouteThreads<32>);
   note_launch();
   if (order && !a.alone) {
-    const size_t bytes = sizeof(uint32_t) * d.experts * (1u + (a.block_rows + 31u) / 32u);
-    launch_pdl(scan_kernel, (d.experts + 31u) / 32u, 1024, 0, s, a);
-    note_launch();
+    const size_t bytes = sizeof(uint32_t) * (d.experts * (1u + (a.block_rows + 31u) / 32u) + 2u * a.groups_of_counts * round_up4(d.experts));
+    if (!a.groups_of_counts) {
+      launch_pdl(scan_kernel, (d.experts + 31u) / 32u, 1024, 0, s, a);
+      note_launch();
+    }
     if (bytes > 48u * 1024u) cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     launch_pdl(order_kernel, a.blocks, 1024, bytes, s, a);
     note_launch();
