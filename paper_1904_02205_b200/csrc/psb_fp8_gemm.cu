@@ -1002,6 +1002,12 @@ psb_status launch_gemm_fp8(psb_ctx* ctx, const Fp8GemmArgs& given, void* scratch
   if (each <= (a.experts ? 8u : 16u)) return launch_stream<16>(ctx, a, s);
   if (each <= (a.experts ? 24u : 32u)) return launch_stream<32>(ctx, a, s);
   if (!a.experts && each <= 128u) return launch_stream<64>(ctx, a, s);
+  // More rows too, where tiles leave most SMs idle and the reduction axis is long enough to be cut; us, streamed with 64 rows against tiles of
+  // 128 x 128: 214 x 1885 x 5071 15.1 and 21.9, 145 x 554 x 2774 8.6 and 12.6, 1024 x 512 x 8192 18.1 and 23.9, 256 x 1000 x 2048 8.9 and 9.7,
+  // 512 x 1000 x 2048 10.8 and 9.9.
+  const uint64_t streamed = (uint64_t)((each + 63u) / 64u) * ((a.n + 127u) / 128u), blocks = (a.k + kBlockK - 1u) / kBlockK;
+  if (!a.experts && ((streamed * 2u <= (uint64_t)ctx->sm_count && blocks >= 24u) || (streamed * 4u <= (uint64_t)ctx->sm_count && blocks >= 8u)))
+    return launch_stream<64>(ctx, a, s);
   // Tiles of 256 x 256 by pairs of SMs read half of the bytes per product that single SMs' 128 x 128 do, and take 1.65 times as long a
   // block for twice an SM's work; what counts is the number of rounds of tiles (in halves: a run of an expert ends in the middle of a
   // tile).  us, pairs against singles: 8192^3 523 and 622, 4096^3 90 and 96, 1500 x 1000 x 2048 18.6 and 12.3, 3000 x 2500 x 1000

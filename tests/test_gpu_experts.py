@@ -233,7 +233,7 @@ def check_experts(ctx, a, sa, b, sb, offsets, order, k, out, fill, **how):
 
 
 @pytest.mark.parametrize("experts,rows,n,k", [(1, 1, 1, 1), (4, 3, 128, 128), (8, 40, 200, 300), (3, 300, 130, 256), (16, 100, 256, 1000), (64, 256, 384, 512),
-                                              (5, 1500, 520, 640), (2, 700, 1000, 130), (1024, 500, 64, 128), (7, 2000, 256, 2048)])
+                                              (5, 1500, 520, 640), (2, 700, 1000, 130), (1024, 500, 64, 128), (7, 2000, 256, 2048), (20, 800, 2000, 300), (2, 6000, 2600, 400)])
 @pytest.mark.parametrize("gather", [True, False])
 def test_products_of_experts(ctx, experts, rows, n, k, gather):
     rng = np.random.default_rng(experts + rows)

@@ -80,7 +80,8 @@ def test_strided_input_and_outputs_leave_what_lies_between(ctx, block_rows):
 # -- product ----------------------------------------------------------------------------------------------------------------
 
 SHAPES = [(1, 1, 1), (1, 128, 128), (3, 5, 17), (2, 1000, 2048), (15, 300, 129), (17, 130, 1000), (64, 127, 256), (65, 129, 640), (127, 64, 384),
-          (128, 128, 128), (129, 257, 130), (200, 1000, 2048), (257, 384, 1152), (300, 520, 4096), (513, 260, 72), (1030, 777, 400), (2, 4096, 4096)]
+          (128, 128, 128), (129, 257, 130), (200, 1000, 2048), (257, 384, 1152), (300, 520, 4096), (513, 260, 72), (1030, 777, 400), (2, 4096, 4096),
+          (145, 554, 2774), (3000, 2500, 1000), (2999, 2507, 900)]
 
 
 @pytest.mark.parametrize("m,n,k", SHAPES)
@@ -94,7 +95,7 @@ def test_product(ctx, m, n, k, out):
     check_product(got, *product(a, sa, b, sb), k)
 
 
-@pytest.mark.parametrize("m,n,k", [(5, 70, 300), (150, 200, 300), (700, 600, 300)])
+@pytest.mark.parametrize("m,n,k", [(5, 70, 300), (150, 200, 300), (700, 600, 300), (2700, 2800, 300)])
 @pytest.mark.parametrize("ta,tb", [(E4, E5), (E5, E4), (E5, E5)])
 def test_formats_bias_relu_and_half(ctx, m, n, k, ta, tb):
     rng = np.random.default_rng(m)
@@ -147,7 +148,7 @@ def test_zero_scales_and_zero_codes(ctx):
     assert (got[5] == 0).all() and (got[:, 128:] == 0).all()
 
 
-@pytest.mark.parametrize("m", [1, 70, 600])
+@pytest.mark.parametrize("m", [1, 70, 600, 5000])
 def test_the_same_call_gives_the_same_bits(ctx, m):
     rng = np.random.default_rng(3)
     a, b = codes(rng, m, 2048), codes(rng, 1000, 2048)
