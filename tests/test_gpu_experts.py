@@ -417,3 +417,36 @@ def test_two_streams_route_at_once(ctx):
         for g, w in zip(got, want):
             for key in w:
                 assert torch.equal(g[key], w[key])
+
+
+def test_two_captured_graphs_and_eager_calls_keep_their_scratch_apart(ctx):
+    """Graphs captured on different streams, replayed at once beside eager calls: gathered rows and counts are their own."""
+    rng = np.random.default_rng(13)
+    E, K, H, top_k = 6, 256, 128, 2
+    layers = []
+    for T in (300, 700, 500):
+        x, gate, _, _, w1, w2 = _parts(ctx, rng, T, E, K, H)
+        mask = torch.ones(T, dtype=torch.uint8, device="cuda")
+        layers.append((x, gate, w1, w2, top_k, mask))
+    want = [_layer(ctx, *l)[1].clone() for l in layers]
+    streams, graphs, got = [torch.cuda.Stream() for _ in range(2)], [], []
+    for s, l in zip(streams, layers):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            l[0].float() @ l[1]
+    torch.cuda.synchronize()
+    for s, l in zip(streams, layers):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            got.append(_layer(ctx, *l)[1])
+        graphs.append(g)
+    for _ in range(10):
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        eager = _layer(ctx, *layers[2])[1]
+        torch.cuda.synchronize()
+        assert torch.equal(eager, want[2])
+        for y, w in zip(got, want):
+            assert torch.equal(y, w)
+    ctx.check_device()
