@@ -19,7 +19,10 @@ namespace psb {
 namespace {
 
 constexpr uint32_t kAll = 0xFFFFFFFFu;
-template <int EL> constexpr uint32_t kRouteThreads = EL <= 8 ? 1024u : 256u;
+// (16384 rows over 256 experts in groups, unsorted: 28 us with 768 threads, 30 with 1024 of 64 registers, 31 to 38 with 512; over 512
+// experts 25 us with 512 threads, 41 with 256; 4096 over 1024 experts 15.5 with either, and the scratch of 16 warps with as many groups
+// as experts would pass a block's shared memory)
+template <int EL> constexpr uint32_t kRouteThreads = EL <= 8 ? 768u : EL == 16 ? 512u : 256u;
 constexpr uint32_t kMaxBlockRows = 1024;   // rows of a counting block: 32 words of a bit mask
 // Two fp32 select values are told apart if they differ by more than unit + kRound * (|v| + |w|).  exp is off by 2^-22 and 2^-24 of its argument,
 // relatively, a quotient by 2^-23.  A sigmoid p changes by p (1 - p) of exp's error: 1/4 of 2^-22, 0.23 of 2^-24, and its sum and quotient
@@ -311,17 +314,21 @@ __device__ __forceinline__ bool choose(const RouteArgs& a, const float (&x)[EL],
 }
 
 // The choices of one row in 64 bits, from memory again.  The rare case: its code is met cold, line by line, by the one warp
-// that needs it, while the other warps of the launch finish, so it is short (loops through shared memory, no unrolled copies
-// of exp: 30 us of a launch otherwise).  `keys`: [experts + groups].
+// that needs it, while the other warps of the launch finish, so it is short (loops through shared memory, two copies of exp
+// and not one for each of the lane's experts: 30 us of a launch otherwise).  `keys`: [experts + groups].
 __device__ __noinline__ int choose_exactly(const RouteArgs& a, float xmax, uint32_t t, uint32_t lane, unsigned long long* keys) {
   typedef unsigned long long Key;
   const uint64_t row = (uint64_t)t * a.logit_stride;
   double sum = 0.0;
+  __syncwarp();           // (the groups' strengths of the 32-bit choice have been read)
+  // (the loads together; the lane's own places)
+#pragma unroll 4
+  for (uint32_t e = lane; e < a.experts; e += 32u) keys[e] = (Key)__float_as_uint(load_clean(a, row + e));
 #pragma unroll 1
   for (uint32_t pass = a.sigmoid ? 1u : 0u; pass < 2u; ++pass) {
-#pragma unroll 1
+#pragma unroll 2
     for (uint32_t e = lane; e < a.experts; e += 32u) {
-      const double x = (double)load_clean(a, row + e), v = exp(a.sigmoid ? -x : x - (double)xmax);
+      const double x = (double)__uint_as_float((uint32_t)keys[e]), v = exp(a.sigmoid ? -x : x - (double)xmax);
       if (pass == 0u) {
         if (x == x) sum += v;
       } else {
@@ -338,7 +345,7 @@ __device__ __noinline__ int choose_exactly(const RouteArgs& a, float xmax, uint3
 #pragma unroll 1
     for (uint32_t g = lane; g < a.groups; g += 32u) {
       Key first = 0, second = 0;
-#pragma unroll 1
+#pragma unroll 4
       for (uint32_t j = 0; j < size; ++j) merge_best(first, second, keys[g * size + j], (Key)0);
       group[g] = !first ? (Key)0 : key_of((second && a.group_best > 1u ? value_of(first) + value_of(second) : value_of(first)) + 0.0);
     }
@@ -346,10 +353,10 @@ __device__ __noinline__ int choose_exactly(const RouteArgs& a, float xmax, uint3
 #pragma unroll 1
     for (uint32_t g = lane; g < a.groups; g += 32u) {
       uint32_t before = 0;
-#pragma unroll 1
+#pragma unroll 4
       for (uint32_t o = 0; o < a.groups; ++o) before += (group[o] > group[g] || (group[o] == group[g] && o < g)) ? 1u : 0u;
       if (before >= a.top_groups) {
-#pragma unroll 1
+#pragma unroll 4
         for (uint32_t j = 0; j < size; ++j) keys[g * size + j] = 0;
       }
     }
@@ -360,7 +367,7 @@ __device__ __noinline__ int choose_exactly(const RouteArgs& a, float xmax, uint3
   for (uint32_t j = 0; j < a.top_k; ++j) {
     Key best = 0;
     uint32_t at = 0xFFFFFFFFu;
-#pragma unroll 1
+#pragma unroll 4
     for (uint32_t e = lane; e < a.experts; e += 32u)
       if (keys[e] > best) { best = keys[e]; at = e; }
     const Key top = warp_max(best);

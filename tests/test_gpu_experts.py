@@ -106,6 +106,16 @@ def test_groups(ctx, experts, groups, top_groups, group_best, top_k, score, with
     check_route(ctx, x, top_k, score, bias, groups, top_groups, group_best)
 
 
+@pytest.mark.parametrize("experts", [256, 512, 1024])
+@pytest.mark.parametrize("tokens", [3, 400])
+def test_every_expert_a_group_of_its_own(ctx, experts, tokens):
+    """The largest scratch of a block; rows of coarse logits, most of which are settled in 64 bits."""
+    rng = np.random.default_rng(experts + tokens)
+    x = (np.round(rng.normal(0, 1, size=(tokens, experts)) * 8) / 8).astype(np.float32)
+    check_route(ctx, x, 8, "softmax", None, experts, 20, 2)
+    check_route(ctx, x, 8, "sigmoid", (rng.integers(0, 3, size=experts) / 8).astype(np.float32), experts, 20, 1)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("groups", [1, 4])
 def test_ties_go_to_the_lower_index(ctx, dtype, groups):
