@@ -232,11 +232,13 @@ def _on(t, device, what):
 def _rows(t, multiple=1):
     """Elements between the rows of a matrix whose row elements follow one another."""
     strides, shape = t.stride(), t.shape
-    if strides[-1] == 1 and shape[-2] > 1:
+    if shape[-2] > 1:
+        if strides[-1] != 1 and shape[-1] > 1 or strides[-2] == 0:      # (a stride of 0 is the default to the library)
+            raise ValueError("the elements of a row must follow one another, rows must not share memory")
         return strides[-2]
     if strides[-1] != 1 and shape[-1] > 1:
         raise ValueError("the elements of a row must follow one another")
-    return strides[-2] if shape[-2] > 1 else -(-shape[-1] // multiple) * multiple
+    return -(-shape[-1] // multiple) * multiple
 
 
 def _matrix(rows, cols, dtype, device, pitch=0):
@@ -463,7 +465,7 @@ class Context:
         device = self.device
         _on(x, device, "x")
         rows, cols = x.shape
-        blocks, scale_rows = (cols + 127) // 128, (rows + block_rows - 1) // block_rows
+        blocks, scale_rows = (cols + 127) // 128, rows if block_rows == 1 else (rows + 127) // 128
         if out is None:
             pitch = (cols + 15) & ~15
             codes = _matrix(rows, cols, code_dtype, device, pitch)
@@ -523,6 +525,8 @@ class Context:
                 assert t.dtype == torch.int32 and t.is_contiguous() and t.dim() == 1
         if offsets.shape[0] != experts + 1 or b_scale.shape[0] != experts:
             raise ValueError("one more offset than experts, and scales of each")
+        if experts > 1 and (b.stride(0) == 0 or b_scale.stride(0) == 0):
+            raise ValueError("each expert has a filter and scales of its own")
         head = self._gemm_fp8_head(a, a_scale, b, b_scale, bias, relu, out, m, n, k, rows)
         d = _EXPERTS_BLOCK.pack(*head, experts, rows, b.stride(0) if experts > 1 else 0, b_scale.stride(0) if experts > 1 else 0)
         _check(self.lib.packed_gemm_fp8_experts(self.handle, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(),

@@ -129,3 +129,36 @@ def test_the_binding_wants_rows_in_one_piece():
 def test_the_binding_refuses_tensors_of_another_device():
     with pytest.raises(ValueError):
         B.Context.quantize_fp8(type("X", (), dict(device=torch.device("cuda", 0)))(), torch.zeros(2, 2))
+
+
+def test_the_binding_refuses_rows_on_top_of_one_another():
+    """A stride of 0 means rows that follow one another to the library: an expanded tensor would be read beyond its end."""
+    for t in (torch.zeros(1, 32).expand(4, 32), torch.zeros(1, 1).expand(4, 1), torch.zeros(2, 1, 16).expand(2, 3, 16)):
+        with pytest.raises(ValueError):
+            B._rows(t)
+
+
+@pytest.mark.parametrize("which", ["b", "b_scale"])
+def test_the_binding_refuses_one_filter_for_all_experts(which):
+    e4 = torch.float8_e4m3fn
+    b, sb = torch.zeros(3, 8, 160).to(e4), torch.ones(3, 1, 2)
+    if which == "b":
+        b = b[:1].expand(3, 8, 160)
+    else:
+        sb = sb[:1].expand(3, 1, 2)
+    with pytest.raises(ValueError):
+        B.Context.gemm_fp8_experts(type("X", (_Ctx,), dict(_gemm_fp8_head=B.Context._gemm_fp8_head))(), torch.zeros(4, 160).to(e4), torch.ones(4, 2),
+                                   b, sb, torch.zeros(4, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("block_rows", [0, 64])
+def test_the_library_sees_other_blocks_than_it_has(block_rows):
+    class Seen(Exception):
+        pass
+
+    def call(*args):
+        raise Seen(B.psb_quantize_desc.from_buffer_copy(args[2]).block_rows)
+    lib = type("L", (), dict(packed_quantize_fp8=staticmethod(call)))
+    with pytest.raises(Seen) as e:
+        B.Context.quantize_fp8(type("X", (_Ctx,), dict(lib=lib))(), torch.zeros(2, 200), block_rows=block_rows, stream=type("S", (), dict(cuda_stream=0)))
+    assert e.value.args[0] == block_rows
