@@ -492,8 +492,9 @@ class Context:
             raise ValueError("out must be [%d, %d]" % (rows, n))
         if bias is not None:
             _on(bias, device, "bias")
-            if bias.dtype != torch.float32 or not bias.is_contiguous() or bias.shape[-1] != n or bias.dim() != b.dim() - 1:
-                raise ValueError("bias must be float32, one for each output")
+            # (the kernels read that of expert e at e * n)
+            if bias.dtype != torch.float32 or not bias.is_contiguous() or bias.shape != b.shape[:-1]:
+                raise ValueError("bias must be float32, one for each output (of each expert)")
         return (_CODE_DT[a.dtype], _CODE_DT[b.dtype], _REAL_DT[out.dtype], m, n, k, 1 if relu else 0, 0, _rows(a, 16), _rows(b, 16),
                 _rows(a_scale), _rows(b_scale), _rows(out), 0 if bias is None else bias.data_ptr())
 

@@ -162,3 +162,47 @@ def test_the_library_sees_other_blocks_than_it_has(block_rows):
     with pytest.raises(Seen) as e:
         B.Context.quantize_fp8(type("X", (_Ctx,), dict(lib=lib))(), torch.zeros(2, 200), block_rows=block_rows, stream=type("S", (), dict(cuda_stream=0)))
     assert e.value.args[0] == block_rows
+
+
+class _Passed(Exception):
+    """The binding handed its arguments on."""
+
+
+def _stand_in(device="cpu"):
+    """A context whose library only says that it was called, with the arguments."""
+    def call(*args):
+        raise _Passed(*args)
+    names = ("quantize_fp8", "gemm_fp8", "gemm_fp8_experts", "route_experts", "combine_experts")
+    ctx = type("X", (), dict(_gemm_fp8_head=B.Context._gemm_fp8_head))()
+    ctx.device, ctx.handle = torch.device(device), None
+    ctx.lib = type("L", (), {"packed_" + n: staticmethod(call) for n in names})
+    return ctx
+
+
+_STREAM = type("S", (), dict(cuda_stream=0))
+
+
+def _product_of_experts(bias, experts=3, n=8, k=160, **how):
+    e4 = torch.float8_e4m3fn
+    return B.Context.gemm_fp8_experts(_stand_in(), torch.zeros(4, k).to(e4), torch.ones(4, 2), torch.zeros(experts, n, k).to(e4),
+                                      torch.ones(experts, 1, 2), torch.zeros(experts + 1, dtype=torch.int32), bias=bias, stream=_STREAM, **how)
+
+
+@pytest.mark.parametrize("shape", [(1, 8), (2, 8), (0, 8), (4, 8), (3, 1), (8,), (1, 3, 8)])
+def test_the_binding_refuses_biases_of_other_experts(shape):
+    """The kernels read the bias of expert e at e * n: fewer rows than experts would be read past their end."""
+    with pytest.raises(ValueError):
+        _product_of_experts(torch.zeros(shape))
+
+
+def test_the_binding_passes_a_bias_for_each_expert():
+    with pytest.raises(_Passed):
+        _product_of_experts(torch.zeros(3, 8))
+
+
+@pytest.mark.parametrize("shape", [(1, 8), (7,), (9,), (1,), (0,)])
+def test_the_binding_refuses_other_biases_of_one_filter(shape):
+    e4 = torch.float8_e4m3fn
+    with pytest.raises(ValueError):
+        B.Context.gemm_fp8(_stand_in(), torch.zeros(4, 160).to(e4), torch.ones(4, 2), torch.zeros(8, 160).to(e4), torch.ones(1, 2),
+                           bias=torch.zeros(shape), stream=_STREAM)
