@@ -24,6 +24,13 @@ constexpr uint32_t kAll = 0xFFFFFFFFu;
 // as experts would pass a block's shared memory)
 template <int EL> constexpr uint32_t kRouteThreads = EL <= 8 ? 768u : EL == 16 ? 512u : 256u;
 constexpr uint32_t kMaxBlockRows = 1024;   // rows of a counting block: 32 words of a bit mask
+// The most dynamic shared memory of a launch, which every launch sets as its kernel's limit: the limit belongs to a kernel on a device, not to a
+// context, and host threads that set each call's own size would lower it under one another's launches.
+constexpr int kMaxSmem = 160 * 1024;
+template <int EL> constexpr uint32_t kMostRouteSmem = kRouteThreads<EL> / 32u * (2u * 32u * EL) * 8u + 3u * 32u * EL * 4u;   // (as many groups as experts)
+static_assert(kMostRouteSmem<8> <= kMaxSmem && kMostRouteSmem<16> <= kMaxSmem && kMostRouteSmem<32> <= kMaxSmem, "scratch of the warps");
+static_assert(1024u * (1u + kMaxBlockRows / 32u) * 4u <= kMaxSmem, "bits of a block's rows, counts in words");
+static_assert(1024u * (1u + 8u) * 4u + 2u * 4u * 1024u * 4u <= kMaxSmem, "bits of a block's rows, counts in bytes");
 // Two fp32 select values are told apart if they differ by more than unit + kRound * (|v| + |w|).  exp is off by 2^-22 and 2^-24 of its argument,
 // relatively, a quotient by 2^-23.  A sigmoid p changes by p (1 - p) of exp's error: 1/4 of 2^-22, 0.23 of 2^-24, and its sum and quotient
 // round: below 3e-7 in all.  A softmax has the errors of exp twice, the quotient's and those of the sum of `el` numbers a lane and five
@@ -781,7 +788,7 @@ cudaError_t launch_route(const void* logits, const float* bias, const uint8_t* m
   const uint32_t ints = d.experts * (a.alone ? 1u + (a.block_rows + 31u) / 32u : 1u);
   auto go = [&](auto kernel, uint32_t threads) {
     const size_t smem = ((ints * 4u + 15u) & ~15u) + sizeof(double) * (threads / 32u) * (d.experts + d.groups);
-    if (smem > 48u * 1024u) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (smem > 48u * 1024u) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
     launch_pdl(kernel, a.blocks, threads, smem, s, a);
   };
   if (el == 1u) go(route_kernel<1>, kRouteThreads<1>);
@@ -797,7 +804,7 @@ cudaError_t launch_route(const void* logits, const float* bias, const uint8_t* m
       launch_pdl(scan_kernel, (d.experts + 31u) / 32u, 1024, 0, s, a);
       note_launch();
     }
-    if (bytes > 48u * 1024u) cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (bytes > 48u * 1024u) cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
     launch_pdl(order_kernel, a.blocks, 1024, bytes, s, a);
     note_launch();
   }
