@@ -786,29 +786,32 @@ cudaError_t launch_route(const void* logits, const float* bias, const uint8_t* m
   const uint32_t size = d.experts / d.groups, lanes = size / el;
   a.lanes_per_group = size % el == 0u && (lanes & (lanes - 1u)) == 0u ? lanes : 0u;
   const uint32_t ints = d.experts * (a.alone ? 1u + (a.block_rows + 31u) / 32u : 1u);
-  auto go = [&](auto kernel, uint32_t threads) {
-    const size_t smem = ((ints * 4u + 15u) & ~15u) + sizeof(double) * (threads / 32u) * (d.experts + d.groups);
-    if (smem > 48u * 1024u) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
-    launch_pdl(kernel, a.blocks, threads, smem, s, a);
+  // (a launch that fails is the last: those behind it take the choices as indices)
+  auto go = [&](auto kernel, uint32_t blocks, uint32_t threads, size_t smem) {
+    cudaError_t e = cudaSuccess;
+    if (smem > 48u * 1024u) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+    if (e == cudaSuccess) e = launch_pdl(kernel, blocks, threads, smem, s, a);
+    const cudaError_t last = cudaGetLastError();
+    if (e == cudaSuccess) e = last;
+    if (e == cudaSuccess) note_launch();
+    return e;
   };
-  if (el == 1u) go(route_kernel<1>, kRouteThreads<1>);
-  else if (el == 2u) go(route_kernel<2>, kRouteThreads<2>);
-  else if (el == 4u) go(route_kernel<4>, kRouteThreads<4>);
-  else if (el == 8u) go(route_kernel<8>, kRouteThreads<8>);
-  else if (el == 16u) go(route_kernel<16>, kRouteThreads<16>);
-  else go(route_kernel<32>, kRouteThreads<32>);
-  note_launch();
-  if (order && !a.alone) {
-    const size_t bytes = sizeof(uint32_t) * (d.experts * (1u + (a.block_rows + 31u) / 32u) + 2u * a.groups_of_counts * round_up4(d.experts));
-    if (!a.groups_of_counts) {
-      launch_pdl(scan_kernel, (d.experts + 31u) / 32u, 1024, 0, s, a);
-      note_launch();
-    }
-    if (bytes > 48u * 1024u) cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
-    launch_pdl(order_kernel, a.blocks, 1024, bytes, s, a);
-    note_launch();
+  auto route = [&](auto kernel, uint32_t threads) {
+    return go(kernel, a.blocks, threads, ((ints * 4u + 15u) & ~15u) + sizeof(double) * (threads / 32u) * (d.experts + d.groups));
+  };
+  cudaError_t e = el == 1u    ? route(route_kernel<1>, kRouteThreads<1>)
+                  : el == 2u  ? route(route_kernel<2>, kRouteThreads<2>)
+                  : el == 4u  ? route(route_kernel<4>, kRouteThreads<4>)
+                  : el == 8u  ? route(route_kernel<8>, kRouteThreads<8>)
+                  : el == 16u ? route(route_kernel<16>, kRouteThreads<16>)
+                              : route(route_kernel<32>, kRouteThreads<32>);
+  if (e == cudaSuccess && order && !a.alone) {
+    if (!a.groups_of_counts) e = go(scan_kernel, (d.experts + 31u) / 32u, 1024, 0);
+    if (e == cudaSuccess)
+      e = go(order_kernel, a.blocks, 1024,
+             sizeof(uint32_t) * (d.experts * (1u + (a.block_rows + 31u) / 32u) + 2u * a.groups_of_counts * round_up4(d.experts)));
   }
-  return cudaGetLastError();
+  return e;
 }
 
 cudaError_t launch_combine(const void* y, const float* weights, const int32_t* slot, const psb_combine_desc& d, void* out,

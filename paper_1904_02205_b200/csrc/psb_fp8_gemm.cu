@@ -985,7 +985,8 @@ psb_status launch_gemm_fp8(psb_ctx* ctx, const Fp8GemmArgs& given, void* scratch
     g.scale_stride = a.a_scale_stride;
     g.err = ctx->err_dev;
     const uint64_t want = ((uint64_t)a.rows * (g.pieces + (g.k_blocks + 3u) / 4u) + 255u) / 256u;
-    launch_pdl(gather_rows_kernel, (uint32_t)(want < kSms * 16u ? want : kSms * 16u), 256, 0, s, g);
+    const cudaError_t e = launch_pdl(gather_rows_kernel, (uint32_t)(want < kSms * 16u ? want : kSms * 16u), 256, 0, s, g), last = cudaGetLastError();
+    if (e != cudaSuccess || last != cudaSuccess) return PSB_ERR_CUDA;      // (there are no rows for the product to read)
     note_launch();
     a.a = g.to;
     a.a_scale = g.scale_to;
