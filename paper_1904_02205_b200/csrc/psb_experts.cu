@@ -129,18 +129,22 @@ __device__ __forceinline__ void load_logits(const RouteArgs& a, uint32_t t, uint
 }
 
 // Two experts of a row, e chosen before o by fp32 values: 1 if that is right, -1 if the other way round is, 0 if it takes the whole row.
-__device__ __noinline__ int exact_order(const RouteArgs& a, uint32_t t, uint32_t e, uint32_t o) {
+__device__ __noinline__ int exact_order(const RouteArgs& a, float xmax, uint32_t t, uint32_t e, uint32_t o) {
   const uint64_t row = (uint64_t)t * a.logit_stride;
   const float x = load_clean(a, row + e), y = load_clean(a, row + o);
   const float b = a.bias ? __ldca(a.bias + e) : 0.0f, c = a.bias ? __ldca(a.bias + o) : 0.0f;
   const int by_index = e < o ? 1 : -1;
   if (b == c && x == y) return by_index;
-  if (!a.bias) {
-    if (x > y) return 1;
-    if (!a.sigmoid) return -1;
-  } else if (!a.sigmoid) {
-    return 0;
+  if (!a.sigmoid) {
+    if (a.bias) return 0;
+    // The scores are monotone in the logits, but in 64 bits they may be equal (0 from 745 below the largest logit on; arguments of exp that round to
+    // the same), and then the index counts.  exp of more than -700, divided by at most 1024, is a normal number, its argument is off by
+    // 2^-44 at most and the score by as much: logits that are 1e-9 apart have different scores.
+    const int by_logit = x > y ? 1 : -1;
+    const double low = (double)fminf(x, y), high = (double)fmaxf(x, y);
+    return by_logit == by_index || (low - (double)xmax > -700.0 && high - low > 1e-9) ? by_logit : 0;
   }
+  if (!a.bias && x > y && by_index > 0) return 1;
   double v[2];
 #pragma unroll 1
   for (int i = 0; i < 2; ++i) v[i] = 1.0 / (1.0 + exp(-(double)(i ? y : x))) + (double)(i ? c : b);
@@ -304,7 +308,7 @@ __device__ __forceinline__ bool choose(const RouteArgs& a, const float (&x)[EL],
       // if its neighbours are certain.  Two in doubt at the border: others behind them may be as close, so the whole row is done again.
       bool swap = false;
       if (((doubts >> lane) & 1u) && lane < a.top_k) {
-        const int order = exact_order(a, t, (uint32_t)my_id, (uint32_t)other_id);
+        const int order = exact_order(a, xmax, t, (uint32_t)my_id, (uint32_t)other_id);
         swap = order < 0;
         const bool border = lane == a.top_k - 1u && ((doubts >> lane >> 1) & 1u);
         if (order == 0 || border || (swap && (((doubts >> 1) | (doubts << 1)) >> lane & 1u))) sure = false;

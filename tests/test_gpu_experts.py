@@ -460,3 +460,21 @@ def test_two_captured_graphs_and_eager_calls_keep_their_scratch_apart(ctx):
         for y, w in zip(got, want):
             assert torch.equal(y, w)
     ctx.check_device()
+
+
+@pytest.mark.parametrize("experts,groups", [(64, 4), (60, 3), (512, 8)])
+@pytest.mark.parametrize("top_k", [2, 3, 4])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_scores_that_are_equal_in_64_bits_go_by_the_index(ctx, experts, groups, top_k, score):
+    """In groups the scores count, not the logits: those that 64 bits hold as 0 or as the same number are ties, whichever way a row's
+    comparisons take."""
+    rows = [{10: 0.0, 3: -900.0, 5: -800.0}, {10: 0.0, 3: -1e9, 5: -800.0, 30: -3.0}, {10: 0.0, 3: -720.0, 5: -710.0}, {10: 4.0, 3: 0.0, 5: 1e-20},
+            {40: 2.0, 3: 1e-25, 5: -1e-25, 9: 1.0}, {10: 0.0, 41: -800.0, 5: -900.0}, {10: 0.0, 3: -3.4e38, 5: -1e30}, {3: -50.0, 5: -60.0, 7: -20.0},
+            {10: 0.0, 3: -900.0, 5: -800.0, 44: -1000.0, 45: -1e5}, {10: 0.0, 3: 2.0 ** -24, 5: 2.0 ** -23},
+            {10: 50.0, 3: 40.0, 5: 60.0, 41: 45.0}, {3: -1e-20, 5: 1e-20, 10: -1e-30, 41: 1e-19}]
+    x = np.full((len(rows), experts), -np.inf, np.float32)
+    for t, row in enumerate(rows):
+        for e, v in row.items():
+            x[t, e] = v
+    for top_groups in (groups, groups - 1):
+        check_route(ctx, x, top_k, score, None, groups, top_groups, 2)
