@@ -445,7 +445,10 @@ psb_status psb_quantize_fp8(psb_ctx* ctx, const void* x_dev, const psb_quantize_
  * few rows leave SMs idle the blocks are cut into parts, whose sums are added in order: the same call gives the same bits).
  *   a_dev [m][k], b_dev [n][k]   codes; addresses and strides are multiples of 16 (PSB_ERR_INVALID_ARG otherwise)
  *   a_scale_dev [m][ceil(k / 128)], b_scale_dev [ceil(n / 128)][ceil(k / 128)], bias_dev fp32 [n] or NULL, out_dev [m][n]
- * NaN codes give NaN (with relu too), infinities of PSB_DT_E5M2 follow the arithmetic of the sum. */
+ * The two scales of a block are multiplied first, and rounded to fp32.  Where that product is infinite, PSB_ERR_RANGE is raised
+ * through psb_device_status, and the outputs that it belongs to are unspecified; where it is below 2^-126 it is off by up to 2^-150, and
+ * what the block adds by that times the block's sum.
+ * NaN codes and scales give NaN (with relu too), infinities of PSB_DT_E5M2 follow the arithmetic of the sum. */
 typedef struct {
   uint32_t a_dtype, b_dtype;  /* PSB_DT_E4M3, PSB_DT_E5M2, each */
   uint32_t out_dtype;         /* PSB_DT_F32, PSB_DT_BF16, PSB_DT_F16 */

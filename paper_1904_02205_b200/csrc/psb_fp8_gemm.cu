@@ -4,7 +4,8 @@
 //
 // The scales are arbitrary fp32 numbers, so the tensor cores can add up one block of 128 only; S_b goes from tensor
 // memory to registers, where the running sum is kept in fp32: one fma per output and block, 1/128 of the MMA's
-// multiply-adds on pipes of 1/64 of its rate.
+// multiply-adds on pipes of 1/64 of its rate.  sa sb is rounded to fp32 before it meets S_b, by a warp that has the time for it (the sums have none
+// for a second multiplication): below 2^-126 that costs bits, and a product that is infinite is reported (PSB_ERR_RANGE).
 //
 // Many rows (gemm_fp8_kernel): one persistent CTA an SM, or a pair of SMs on one tile (cta_group::2).  Warps of their own copy a, copy
 // b, issue the MMAs and multiply the scales; eight warps add up a block of 128 or 256 columns out of one TMEM buffer while the
@@ -448,6 +449,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
       constexpr uint32_t kHalves = BN / 128, kAtOnce = BN == 128 ? 32 : 16;
       const uint32_t kb_off = lane & 7u, r_off = lane >> 3;
       uint32_t cb = 0, cph = 0;
+      float most = 0.0f;          // the largest product (a NaN does not count)
 #pragma unroll 1
       for (uint32_t t = t0; t < tiles && !failed; t += step) {
         const GemmTile tile = tile_at<TM, BN>(p, t, first, offsets);
@@ -467,8 +469,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
             for (uint32_t i = 0; i < kAtOnce; ++i) v[i] = __ldcg(p.g.a_scale + (uint64_t)min(row + r0 + 4u * i, last) * p.g.a_scale_stride + kb);
 #pragma unroll
             for (uint32_t i = 0; i < kAtOnce; ++i) {
-              to[r0 + 4u * i] = v[i] * b0;
-              if (kHalves == 2u) to[kScaleBlocks * kScaleRow + r0 + 4u * i] = v[i] * b1;
+              const float q = v[i] * b0;
+              to[r0 + 4u * i] = q;
+              most = fmaxf(most, fabsf(q));
+              if (kHalves == 2u) {
+                const float q1 = v[i] * b1;
+                to[kScaleBlocks * kScaleRow + r0 + 4u * i] = q1;
+                most = fmaxf(most, fabsf(q1));
+              }
             }
           }
           __syncwarp();
@@ -476,6 +484,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_fp8_kernel(const __grid_
           if (++cb == 2u) { cb = 0; cph ^= 1u; }
         }
       }
+      if (most == INFINITY) atomicOr(p.err, kDevErrRange);
     }
   } else {
     // -------------------------------------------------------------- scaled sums and output
@@ -686,6 +695,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) stream_fp8_kernel(const __gri
     // -------------------------------------------------------------- scales: products for the rows of a, eight blocks at a time
     const uint32_t kb_off = lane & 7u, r_off = lane >> 3;
     uint32_t cb = 0, cph = 0;
+    float most = 0.0f;            // the largest product (a NaN does not count)
 #pragma unroll 1
     for (uint32_t t = t0; t < tiles && !failed; t += step) {
       const GemmTile tile = tile_at<BT, BN>(p, t, first, offsets);
@@ -701,12 +711,17 @@ __global__ void __launch_bounds__(kGemmThreads, 1) stream_fp8_kernel(const __gri
         if (!wait_warp(smem_u32(&ctl->scale_empty[cb]), cph ^ 1u, p.polls)) { failed = true; break; }
         float* to = scales + (cb * kScaleBlocks + kb_off) * BT + r_off;
 #pragma unroll
-        for (uint32_t i = 0; i < BT / 4u; ++i) to[4u * i] = v[i] * b0;
+        for (uint32_t i = 0; i < BT / 4u; ++i) {
+          const float q = v[i] * b0;
+          to[4u * i] = q;
+          most = fmaxf(most, fabsf(q));
+        }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->scale_full[cb]));
         if (++cb == 2u) { cb = 0; cph ^= 1u; }
       }
     }
+    if (most == INFINITY) atomicOr(p.err, kDevErrRange);
   } else {
     // -------------------------------------------------------------- scaled sums: a lane a column of out, a register a row
     const uint32_t quarter = warp & 3u, group = (warp - kFirstSumWarp) >> 2, col = quarter * 32u + lane;
