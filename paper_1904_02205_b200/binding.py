@@ -101,7 +101,7 @@ PSB_OP_CONV2D, PSB_OP_GEMM, PSB_OP_MAXPOOL, PSB_OP_AVGPOOL = 0, 1, 2, 3
 
 # The argument blocks of the calls that a program makes once per layer, packed in one go: filling the ctypes structures
 # field by field took 3 us of a 10 us call.  Values that do not fit their field go through ctypes, which wraps whole numbers and
-# makes infinities of floats.
+# makes infinities of floats (_sized_block: floats alone).
 _EP_FMT = "3QfIIfiiI4x3Q"
 _CONV_BLOCK, _GEMM_BLOCK = struct.Struct("=10I" + _EP_FMT), struct.Struct("=5I4x" + _EP_FMT)
 _SHAPE_BLOCK, _CFG_BLOCK = struct.Struct("=5I"), struct.Struct("=Q8I")
@@ -119,6 +119,16 @@ def _block(packer, ctype, head, ep=()):
         return packer.pack(*head, *ep)
     except (struct.error, OverflowError):
         return bytes(ctype(*head, psb_epilogue(*ep)) if ep else ctype(*head))
+
+
+def _sized_block(packer, ctype, head):
+    """For the calls whose sizes are those of tensors: 2^32 + 5 rows are refused, not taken for five."""
+    try:
+        return packer.pack(*head)
+    except OverflowError:                   # a factor beyond fp32 becomes an infinity
+        return bytes(ctype(*head))
+    except struct.error as e:
+        raise ValueError("a size does not fit its field: %s" % e) from None
 
 _lib = None
 
@@ -476,7 +486,7 @@ class Context:
             _on(codes, device, "codes"), _on(scales, device, "scales")
             assert codes.shape == x.shape and scales.dtype == torch.float32 and tuple(scales.shape) == (scale_rows, blocks)
             strides = (_rows(codes), _rows(scales))
-        d = _block(_QUANT_BLOCK, psb_quantize_desc, (_REAL_DT[x.dtype], _CODE_DT[codes.dtype], rows, cols, block_rows, 0, _rows(x)) + strides)
+        d = _sized_block(_QUANT_BLOCK, psb_quantize_desc, (_REAL_DT[x.dtype], _CODE_DT[codes.dtype], rows, cols, block_rows, 0, _rows(x)) + strides)
         _check(self.lib.packed_quantize_fp8(self.handle, x.data_ptr(), d, codes.data_ptr(), scales.data_ptr(), _stream(stream)),
                "psb_quantize_fp8")
         return codes, scales
@@ -504,7 +514,7 @@ class Context:
         (m, k), (n, _) = a.shape, b.shape
         if out is None:
             out = _matrix(m, n, out_dtype, self.device)
-        d = _GEMM_FP8_BLOCK.pack(*self._gemm_fp8_head(a, a_scale, b, b_scale, bias, relu, out, m, n, k, m))
+        d = _sized_block(_GEMM_FP8_BLOCK, psb_gemm_fp8_desc, self._gemm_fp8_head(a, a_scale, b, b_scale, bias, relu, out, m, n, k, m))
         _check(self.lib.packed_gemm_fp8(self.handle, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), out.data_ptr(), d,
                                         _stream(stream)), "psb_gemm_fp8")
         return out
@@ -529,7 +539,8 @@ class Context:
         if experts > 1 and (b.stride(0) == 0 or b_scale.stride(0) == 0):
             raise ValueError("each expert has a filter and scales of its own")
         head = self._gemm_fp8_head(a, a_scale, b, b_scale, bias, relu, out, m, n, k, rows)
-        d = _EXPERTS_BLOCK.pack(*head, experts, rows, b.stride(0) if experts > 1 else 0, b_scale.stride(0) if experts > 1 else 0)
+        d = _sized_block(_EXPERTS_BLOCK, psb_gemm_fp8_experts_desc,
+                         head + (experts, rows, b.stride(0) if experts > 1 else 0, b_scale.stride(0) if experts > 1 else 0))
         _check(self.lib.packed_gemm_fp8_experts(self.handle, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(),
                                                 offsets.data_ptr(), 0 if order is None else order.data_ptr(), out.data_ptr(), d,
                                                 _stream(stream)), "psb_gemm_fp8_experts")
@@ -563,7 +574,7 @@ class Context:
             out["order"] = torch.empty_strided((n,), (1,), dtype=torch.int32, device=device)
             out["slot"] = _matrix(tokens, top_k, torch.int32, device)
             offsets, order, slot = out["offsets"].data_ptr(), out["order"].data_ptr(), out["slot"].data_ptr()
-        d = _block(_ROUTE_BLOCK, psb_route_desc, (_REAL_DT[logits.dtype], _SCORES[score], tokens, experts, top_k, groups, top_groups,
+        d = _sized_block(_ROUTE_BLOCK, psb_route_desc, (_REAL_DT[logits.dtype], _SCORES[score], tokens, experts, top_k, groups, top_groups,
                                                   group_best, 1 if renormalise else 0, float(scaling), _rows(logits)))
         _check(self.lib.packed_route_experts(self.handle, logits.data_ptr(), 0 if bias is None else bias.data_ptr(),
                                              0 if token_mask is None else token_mask.data_ptr(), d, ids.data_ptr(), weights.data_ptr(), offsets,
@@ -587,7 +598,7 @@ class Context:
             _on(out, self.device, "out")
             if out.shape != (tokens, n):
                 raise ValueError("out must be [%d, %d]" % (tokens, n))
-        d = _block(_COMBINE_BLOCK, psb_combine_desc, (_REAL_DT[y.dtype], _REAL_DT[out.dtype], tokens, top_k, n, rows, _rows(y), _rows(out)))
+        d = _sized_block(_COMBINE_BLOCK, psb_combine_desc, (_REAL_DT[y.dtype], _REAL_DT[out.dtype], tokens, top_k, n, rows, _rows(y), _rows(out)))
         _check(self.lib.packed_combine_experts(self.handle, y.data_ptr(), weights.data_ptr(), slot.data_ptr(), d, out.data_ptr(),
                                                _stream(stream)), "psb_combine_experts")
         return out

@@ -206,3 +206,37 @@ def test_the_binding_refuses_other_biases_of_one_filter(shape):
     with pytest.raises(ValueError):
         B.Context.gemm_fp8(_stand_in(), torch.zeros(4, 160).to(e4), torch.ones(4, 2), torch.zeros(8, 160).to(e4), torch.ones(1, 2),
                            bias=torch.zeros(shape), stream=_STREAM)
+
+
+def _meta(*shape, dtype=torch.float32):
+    return torch.empty(shape, dtype=dtype, device="meta")
+
+
+_MANY = (1 << 32) + 5
+
+
+@pytest.mark.parametrize("call", [
+    lambda c: B.Context.quantize_fp8(c, _meta(_MANY, 1), stream=_STREAM),
+    lambda c: B.Context.quantize_fp8(c, _meta(1, _MANY), stream=_STREAM),
+    lambda c: B.Context.quantize_fp8(c, _meta(4, 4), block_rows=_MANY, stream=_STREAM),
+    lambda c: B.Context.gemm_fp8(c, _meta(_MANY, 16, dtype=torch.float8_e4m3fn), _meta(_MANY, 1), _meta(4, 16, dtype=torch.float8_e4m3fn), _meta(1, 1),
+                                 stream=_STREAM),
+    lambda c: B.Context.gemm_fp8_experts(c, _meta(4, 16, dtype=torch.float8_e4m3fn), _meta(4, 1), _meta(2, 4, 16, dtype=torch.float8_e4m3fn),
+                                         _meta(2, 1, 1), _meta(3, dtype=torch.int32), order=_meta(_MANY, dtype=torch.int32), stream=_STREAM),
+    lambda c: B.Context.route_experts(c, _meta(_MANY, 4), 1, stream=_STREAM),
+    lambda c: B.Context.route_experts(c, _meta(4, 4), 1, groups=(1 << 32) + 1, stream=_STREAM),
+    lambda c: B.Context.route_experts(c, _meta(4, 4), 1, top_groups=1 - (1 << 32), stream=_STREAM),
+    lambda c: B.Context.combine_experts(c, _meta(_MANY, 4), _meta(4, 2), _meta(4, 2, dtype=torch.int32), stream=_STREAM),
+    lambda c: B.Context.combine_experts(c, _meta(8, 1), _meta(_MANY, 1), _meta(_MANY, 1, dtype=torch.int32), stream=_STREAM)])
+def test_the_binding_refuses_sizes_that_do_not_fit_their_field(call):
+    """2^32 + 5 rows are not five."""
+    with pytest.raises(ValueError):
+        call(_stand_in("meta"))
+
+
+def test_factors_beyond_fp32_become_infinities():
+    seen = []
+    ctx = _stand_in()
+    ctx.lib.packed_route_experts = staticmethod(lambda *a: seen.append(B.psb_route_desc.from_buffer_copy(a[4]).scaling) or 0)
+    B.Context.route_experts(ctx, torch.zeros(2, 4), 1, scaling=1e39, stream=_STREAM)
+    assert seen == [float("inf")]
