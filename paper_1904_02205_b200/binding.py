@@ -496,7 +496,7 @@ class Context:
         if a.device != device or a_scale.device != device or b.device != device or b_scale.device != device or out.device != device:
             raise ValueError("a tensor is on another device than the context (%s)" % device)
         assert a_scale.dtype == b_scale.dtype == torch.float32
-        if b.shape[-1] != k or a_scale.shape != (m, blocks) or b_scale.shape[-2:] != ((n + 127) // 128, blocks):
+        if b.shape[-1] != k or a_scale.shape != (m, blocks) or b_scale.shape != b.shape[:-2] + ((n + 127) // 128, blocks):
             raise ValueError("codes and scales do not fit together")
         if out.shape != (rows, n):
             raise ValueError("out must be [%d, %d]" % (rows, n))

@@ -240,3 +240,19 @@ def test_factors_beyond_fp32_become_infinities():
     ctx.lib.packed_route_experts = staticmethod(lambda *a: seen.append(B.psb_route_desc.from_buffer_copy(a[4]).scaling) or 0)
     B.Context.route_experts(ctx, torch.zeros(2, 4), 1, scaling=1e39, stream=_STREAM)
     assert seen == [float("inf")]
+
+
+@pytest.mark.parametrize("shape", [(3, 1, 2), (1, 1, 2), (0, 1, 2), (2,)])
+def test_the_binding_refuses_scales_of_other_filters(shape):
+    """One filter has one matrix of scales: of several, the first alone would count."""
+    e4 = torch.float8_e4m3fn
+    with pytest.raises(ValueError):
+        B.Context.gemm_fp8(_stand_in(), torch.zeros(4, 160).to(e4), torch.ones(4, 2), torch.zeros(8, 160).to(e4), torch.ones(shape), stream=_STREAM)
+
+
+@pytest.mark.parametrize("shape", [(2, 1, 2), (0, 1, 2), (4, 1, 2), (3, 2, 2)])
+def test_the_binding_refuses_scales_of_other_experts(shape):
+    e4 = torch.float8_e4m3fn
+    with pytest.raises(ValueError):
+        B.Context.gemm_fp8_experts(_stand_in(), torch.zeros(4, 160).to(e4), torch.ones(4, 2), torch.zeros(3, 8, 160).to(e4), torch.ones(shape),
+                                   torch.zeros(4, dtype=torch.int32), stream=_STREAM)
