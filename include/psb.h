@@ -468,7 +468,8 @@ psb_status psb_gemm_fp8(psb_ctx* ctx, const uint8_t* a_dev, const float* a_scale
  *   b [experts][n][k], b_scale [experts][ceil(n / 128)][ceil(k / 128)], bias [experts][n] or NULL; experts are
  *   b_expert_stride, b_scale_expert_stride elements apart (0: rows x stride), biases n.
  * experts <= 1024.  Offsets that decrease or leave [0, rows] and rows that a does not have raise PSB_ERR_RANGE through
- * psb_device_status; their outputs are unspecified, and nothing outside the tensors is touched. */
+ * psb_device_status; their outputs are unspecified (with offsets that decrease, out is left as it was), and nothing outside the tensors is
+ * touched. */
 typedef struct {
   psb_gemm_fp8_desc gemm;
   uint32_t experts, rows;

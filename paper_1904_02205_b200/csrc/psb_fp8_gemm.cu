@@ -86,7 +86,8 @@ struct GemmTile {
   uint32_t expert, row, row_end, n0;
 };
 
-// The experts' runs, as checked: offsets cut to the rows that there are, a run that is none counts as empty.  By the whole block.
+// The experts' runs, as checked: offsets cut to the rows that there are; where they decrease there are no runs at all (runs that share rows could be
+// more tiles than 32 bits count).  By the whole block.
 template <uint32_t TM>
 __device__ __forceinline__ void find_runs(const GemmParams& p, uint32_t* offsets, uint32_t* first, uint32_t* tiles) {
   const uint32_t lane = threadIdx.x & 31u;
@@ -98,11 +99,12 @@ __device__ __forceinline__ void find_runs(const GemmParams& p, uint32_t* offsets
   __syncthreads();
   if (threadIdx.x < 32u) {
     uint32_t carry = 0;
+    bool falls = false;
     for (uint32_t e0 = 0; e0 < p.g.experts; e0 += 32u) {
       const uint32_t e = e0 + lane;
       uint32_t mine = 0;
       if (e < p.g.experts) {
-        if (offsets[e + 1u] < offsets[e]) atomicOr(p.err, kDevErrRange);
+        if (offsets[e + 1u] < offsets[e]) falls = true;
         else mine = (offsets[e + 1u] - offsets[e] + TM - 1u) / TM * p.n_tiles;
       }
       uint32_t up = mine;
@@ -113,6 +115,10 @@ __device__ __forceinline__ void find_runs(const GemmParams& p, uint32_t* offsets
       }
       if (e < p.g.experts) first[e] = carry + up - mine;
       carry += __shfl_sync(0xFFFFFFFFu, up, 31);
+    }
+    if (__any_sync(0xFFFFFFFFu, falls)) {
+      carry = 0;
+      if (lane == 0) atomicOr(p.err, kDevErrRange);
     }
     if (lane == 0) first[p.g.experts] = *tiles = carry;
   }

@@ -478,3 +478,29 @@ def test_scores_that_are_equal_in_64_bits_go_by_the_index(ctx, experts, groups, 
             x[t, e] = v
     for top_groups in (groups, groups - 1):
         check_route(ctx, x, top_k, score, None, groups, top_groups, 2)
+
+
+@pytest.mark.parametrize("rows", [12, 64, 300, 4000])
+@pytest.mark.parametrize("gather", [True, False])
+def test_offsets_that_decrease_are_no_runs_at_all(ctx, rows, gather):
+    """Runs that share rows could be more tiles than 32 bits count."""
+    import paper_1904_02205_b200 as psb
+
+    rng = np.random.default_rng(rows)
+    experts, n, k = 40, 300, 1200
+    a, b = codes(rng, rows, k), codes(rng, n, k, batch=experts)
+    sa, sb = scales(rng, rows, up(k, 128)), scales(rng, experts, up(n, 128), up(k, 128))
+    order = torch.arange(rows, dtype=torch.int32, device="cuda") if gather else None
+    for late in (False, True):
+        offsets = torch.full((experts + 1,), rows, dtype=torch.int32)
+        offsets[0] = 0
+        if late:
+            offsets[-2] = 0
+        else:
+            offsets[2::2] = 0
+            offsets[-1] = rows
+        out = torch.full((rows, n), -5.0, device="cuda")
+        ctx.gemm_fp8_experts(a, sa, b, sb, offsets.cuda(), order=order, out=out)
+        assert ctx.device_status() == psb.PSB_ERR_RANGE
+        assert (out == -5.0).all()
+    assert ctx.device_status() == psb.PSB_OK
