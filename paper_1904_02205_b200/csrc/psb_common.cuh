@@ -230,6 +230,13 @@ inline cudaError_t launch_pdl(K kernel, dim3 grid, dim3 block, size_t smem, cuda
 // every kernel launch of the library is counted (process-wide), for throughput reports
 void note_launch();
 unsigned long long launches_so_far();
+// The status of a launch, counted if there was one.  It is the launch's own: the runtime's last error may be that of an earlier call, and is not
+// left to the next one.
+inline cudaError_t launched(cudaError_t e) {
+  if (e == cudaSuccess) note_launch();
+  else cudaGetLastError();
+  return e;
+}
 
 // host-side launchers (defined in the .cu files)
 cudaError_t launch_sampler(const float* w_dev, psb_weights* wt, uint32_t* err_dev, cudaStream_t s);

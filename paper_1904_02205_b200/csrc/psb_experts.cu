@@ -736,15 +736,15 @@ __global__ void __launch_bounds__(256, 4) combine_kernel(const CombineArgs a) {
 }
 
 template <typename TI, typename TO>
-void launch_combine_as(const CombineArgs& a, cudaStream_t s) {
-  if (a.pieces == 2u) launch_pdl(combine_kernel<TI, TO, 2>, a.tokens * a.row_blocks, a.threads, 0, s, a);
-  else launch_pdl(combine_kernel<TI, TO, 1>, a.tokens * a.row_blocks, a.threads, 0, s, a);
+cudaError_t launch_combine_as(const CombineArgs& a, cudaStream_t s) {
+  return launched(a.pieces == 2u ? launch_pdl(combine_kernel<TI, TO, 2>, a.tokens * a.row_blocks, a.threads, 0, s, a)
+                                 : launch_pdl(combine_kernel<TI, TO, 1>, a.tokens * a.row_blocks, a.threads, 0, s, a));
 }
 template <typename TI>
-void launch_combine_from(const CombineArgs& a, uint32_t out_dtype, cudaStream_t s) {
-  if (out_dtype == PSB_DT_F32) launch_combine_as<TI, float>(a, s);
-  else if (out_dtype == PSB_DT_BF16) launch_combine_as<TI, __nv_bfloat16>(a, s);
-  else launch_combine_as<TI, __half>(a, s);
+cudaError_t launch_combine_from(const CombineArgs& a, uint32_t out_dtype, cudaStream_t s) {
+  if (out_dtype == PSB_DT_F32) return launch_combine_as<TI, float>(a, s);
+  if (out_dtype == PSB_DT_BF16) return launch_combine_as<TI, __nv_bfloat16>(a, s);
+  return launch_combine_as<TI, __half>(a, s);
 }
 
 }  // namespace
@@ -794,11 +794,7 @@ cudaError_t launch_route(const void* logits, const float* bias, const uint8_t* m
   auto go = [&](auto kernel, uint32_t blocks, uint32_t threads, size_t smem) {
     cudaError_t e = cudaSuccess;
     if (smem > 48u * 1024u) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
-    if (e == cudaSuccess) e = launch_pdl(kernel, blocks, threads, smem, s, a);
-    const cudaError_t last = cudaGetLastError();
-    if (e == cudaSuccess) e = last;
-    if (e == cudaSuccess) note_launch();
-    return e;
+    return launched(e == cudaSuccess ? launch_pdl(kernel, blocks, threads, smem, s, a) : e);
   };
   auto route = [&](auto kernel, uint32_t threads) {
     return go(kernel, a.blocks, threads, ((ints * 4u + 15u) & ~15u) + sizeof(double) * (threads / 32u) * (d.experts + d.groups));
@@ -839,11 +835,9 @@ cudaError_t launch_combine(const void* y, const float* weights, const int32_t* s
   a.threads = share < 256u ? round_up(share, 32u) : 256u;
   a.row_blocks = (share + a.threads - 1u) / a.threads;
   a.wide = (((uintptr_t)y | (uintptr_t)out | d.y_stride * in | d.out_stride * to) & 15u) == 0u;
-  if (d.in_dtype == PSB_DT_F32) launch_combine_from<float>(a, d.out_dtype, s);
-  else if (d.in_dtype == PSB_DT_BF16) launch_combine_from<__nv_bfloat16>(a, d.out_dtype, s);
-  else launch_combine_from<__half>(a, d.out_dtype, s);
-  note_launch();
-  return cudaGetLastError();
+  if (d.in_dtype == PSB_DT_F32) return launch_combine_from<float>(a, d.out_dtype, s);
+  if (d.in_dtype == PSB_DT_BF16) return launch_combine_from<__nv_bfloat16>(a, d.out_dtype, s);
+  return launch_combine_from<__half>(a, d.out_dtype, s);
 }
 
 }  // namespace psb

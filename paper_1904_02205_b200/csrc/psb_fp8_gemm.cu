@@ -918,7 +918,7 @@ uint64_t row_tiles(const Fp8GemmArgs& a, uint32_t height) {
 
 template <typename K>
 psb_status launch_gemm(K kernel, uint32_t grid, uint32_t cluster, size_t smem, const GemmMaps& maps, const GemmParams& p, cudaStream_t s) {
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget) != cudaSuccess) return PSB_ERR_CUDA;
+  const cudaError_t limit = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget);
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -932,9 +932,7 @@ psb_status launch_gemm(K kernel, uint32_t grid, uint32_t cluster, size_t smem, c
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 1u ? 2 : 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, maps, p);
-  note_launch();
-  return e != cudaSuccess || cudaGetLastError() != cudaSuccess ? PSB_ERR_CUDA : PSB_OK;
+  return launched(limit == cudaSuccess ? cudaLaunchKernelEx(&cfg, kernel, maps, p) : limit) == cudaSuccess ? PSB_OK : PSB_ERR_CUDA;
 }
 
 uint32_t runs_bytes(const Fp8GemmArgs& a) { return a.experts ? (a.experts + 1u) * 8u : 0u; }
@@ -1006,9 +1004,8 @@ psb_status launch_gemm_fp8(psb_ctx* ctx, const Fp8GemmArgs& given, void* scratch
     g.scale_stride = a.a_scale_stride;
     g.err = ctx->err_dev;
     const uint64_t want = ((uint64_t)a.rows * (g.pieces + (g.k_blocks + 3u) / 4u) + 255u) / 256u;
-    const cudaError_t e = launch_pdl(gather_rows_kernel, (uint32_t)(want < kSms * 16u ? want : kSms * 16u), 256, 0, s, g), last = cudaGetLastError();
-    if (e != cudaSuccess || last != cudaSuccess) return PSB_ERR_CUDA;      // (there are no rows for the product to read)
-    note_launch();
+    if (launched(launch_pdl(gather_rows_kernel, (uint32_t)(want < kSms * 16u ? want : kSms * 16u), 256, 0, s, g)) != cudaSuccess)
+      return PSB_ERR_CUDA;      // (there are no rows for the product to read)
     a.a = g.to;
     a.a_scale = g.scale_to;
     a.a_stride = (uint64_t)g.pieces * 16u;

@@ -209,14 +209,10 @@ __global__ void __launch_bounds__(256) quantize_tile_kernel(const QuantArgs a) {
 }
 
 template <typename T, bool E5M2>
-void launch(const QuantArgs& a, uint32_t block_rows, cudaStream_t s) {
-  if (block_rows == 1u) {
-    const uint64_t want = ((uint64_t)a.rows * a.blocks + 31u) / 32u;
-    launch_pdl(quantize_rows_kernel<T, E5M2>, (uint32_t)(want < kSms * 8u ? want : kSms * 8u), 256, 0, s, a);
-  } else {
-    launch_pdl(quantize_tile_kernel<T, E5M2>, (a.rows + 127u) / 128u * a.blocks, 256, 0, s, a);
-  }
-  note_launch();
+cudaError_t launch(const QuantArgs& a, uint32_t block_rows, cudaStream_t s) {
+  if (block_rows != 1u) return launched(launch_pdl(quantize_tile_kernel<T, E5M2>, (a.rows + 127u) / 128u * a.blocks, 256, 0, s, a));
+  const uint64_t want = ((uint64_t)a.rows * a.blocks + 31u) / 32u;
+  return launched(launch_pdl(quantize_rows_kernel<T, E5M2>, (uint32_t)(want < kSms * 8u ? want : kSms * 8u), 256, 0, s, a));
 }
 
 }  // namespace
@@ -237,10 +233,9 @@ cudaError_t launch_quantize_fp8(const void* x, const psb_quantize_desc& d, uint8
   a.wide_out = (((uintptr_t)codes | d.code_stride) & 15u) == 0u;
   const bool e5 = d.code_dtype == PSB_DT_E5M2;
   a.top = e5 ? 57344.0f : 448.0f;
-  if (d.in_dtype == PSB_DT_F32) e5 ? launch<float, true>(a, d.block_rows, s) : launch<float, false>(a, d.block_rows, s);
-  else if (d.in_dtype == PSB_DT_BF16) e5 ? launch<__nv_bfloat16, true>(a, d.block_rows, s) : launch<__nv_bfloat16, false>(a, d.block_rows, s);
-  else e5 ? launch<__half, true>(a, d.block_rows, s) : launch<__half, false>(a, d.block_rows, s);
-  return cudaGetLastError();
+  if (d.in_dtype == PSB_DT_F32) return e5 ? launch<float, true>(a, d.block_rows, s) : launch<float, false>(a, d.block_rows, s);
+  if (d.in_dtype == PSB_DT_BF16) return e5 ? launch<__nv_bfloat16, true>(a, d.block_rows, s) : launch<__nv_bfloat16, false>(a, d.block_rows, s);
+  return e5 ? launch<__half, true>(a, d.block_rows, s) : launch<__half, false>(a, d.block_rows, s);
 }
 
 }  // namespace psb
