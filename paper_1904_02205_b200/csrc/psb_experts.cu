@@ -31,10 +31,14 @@ template <int EL> constexpr uint32_t kMostRouteSmem = kRouteThreads<EL> / 32u * 
 static_assert(kMostRouteSmem<8> <= kMaxSmem && kMostRouteSmem<16> <= kMaxSmem && kMostRouteSmem<32> <= kMaxSmem, "scratch of the warps");
 static_assert(1024u * (1u + kMaxBlockRows / 32u) * 4u <= kMaxSmem, "bits of a block's rows, counts in words");
 static_assert(1024u * (1u + 8u) * 4u + 2u * 4u * 1024u * 4u <= kMaxSmem, "bits of a block's rows, counts in bytes");
-// Two fp32 select values are told apart if they differ by more than unit + kRound * (|v| + |w|).  exp is off by 2^-22 and 2^-24 of its argument,
-// relatively, a quotient by 2^-23.  A sigmoid p changes by p (1 - p) of exp's error: 1/4 of 2^-22, 0.23 of 2^-24, and its sum and quotient
-// round: below 3e-7 in all.  A softmax has the errors of exp twice, the quotient's and those of the sum of `el` numbers a lane and five
-// levels of lanes, all of them of the row's largest score at most.  Two values, hence twice.  The bias rounds once, 2^-24 of the value.
+// Two fp32 select values are told apart if they differ by more than unit + kRound * (|v| + |w|).  The bounds that CUDA publishes are 2 + 1.173 |z| units
+// in the last place for __expf(z) and 2 for __fdividef, a unit being at most 2^-23 of the number; sums and differences round to half a unit.
+// A sigmoid p is off by p (1 - p) of exp's error, p 2^-24 of the sum's and the quotient's: 2.99e-7 at most.  Two values, hence twice.
+// A softmax, in parts of the row's largest score: exp and its argument's rounding are off by 2.4e-7 at most (at the top; e^-d (2.4 + 2 d) 1e-7 falls), the
+// quotient by 2.4e-7, twice for two values.  The sum's error is common to both values and moves them apart by that part of their difference,
+// hence once: the mean of exp's errors by scores, 2.4e-7 + 2e-7 d n e^-d / (1 + n e^-d) for n scores of e^-d beside the top (d times its quotient is 3.4 at
+// most for 256 experts, 4.5 for 1024), and the roundings of `el` numbers a lane and five levels of lanes.  In all 1.9e-6 for 32 experts, 2.7e-6
+// for 256, 4.3e-6 for 1024, where softmax_unit is 2.3e-6, 3.1e-6 and 6e-6.  The bias rounds once, 2^-24 of the value.
 constexpr float kSigmoidUnit = 6e-7f, kRound = 1.2e-7f;
 __host__ __device__ constexpr float softmax_unit(int el) { return 2.0f * (8e-7f + 6e-8f * (float)(el + 5)); }
 

@@ -504,3 +504,19 @@ def test_offsets_that_decrease_are_no_runs_at_all(ctx, rows, gather):
         assert ctx.device_status() == psb.PSB_ERR_RANGE
         assert (out == -5.0).all()
     assert ctx.device_status() == psb.PSB_OK
+
+
+@pytest.mark.parametrize("experts,below", [(1024, 5.2), (1000, 7.0), (256, 4.0), (64, 2.6), (32, 2.4), (31, 9.0)])
+@pytest.mark.parametrize("groups", [1, "all"])
+def test_near_ties_beside_many_middling_scores(ctx, experts, below, groups):
+    """Scores whose sum is far from the largest of them, which is where the sum's error is largest; the bias brings half of the row's
+    select values within a few units of fp32 of one another."""
+    rng = np.random.default_rng(experts)
+    groups = 1 if groups == 1 else next(g for g in (8, 4, 2, 1) if experts % g == 0)
+    x = np.full((60, experts), -below, np.float32) + rng.normal(0, 0.3, size=(60, experts)).astype(np.float32)
+    x[np.arange(60), rng.integers(0, experts, size=60)] = 0.0
+    x[1:] = x[0] + (rng.integers(-3, 4, size=(59, experts)) * 2.0 ** -22).astype(np.float32)
+    x64 = x[0].astype(np.float64)
+    p = np.exp(x64) / np.exp(x64).sum()
+    bias = np.where(rng.random(experts) < 0.5, 0.75 - p, -0.5).astype(np.float32)
+    check_route(ctx, x, min(8, experts), "softmax", bias, groups, max(1, groups // 2), 2)
