@@ -63,7 +63,8 @@ enum {
   PSB_ERR_CUDA = -5,             /* a CUDA runtime / driver call failed                          */
   PSB_ERR_TIMEOUT = -6,          /* a bounded device-side wait ran out (reported by the device)  */
   PSB_ERR_NONFINITE_WEIGHT = -7, /* a filter holds Inf or NaN (reported by the device)           */
-  PSB_ERR_RANGE = -8             /* an activation exceeds the in_max the caller vouched for
+  PSB_ERR_RANGE = -8             /* an activation exceeds the in_max the caller vouched for, or a
+                                    number that a call reads on the device leaves its range
                                     (reported by the device)                                     */
 };
 

@@ -4,15 +4,16 @@
 //
 // The scales are arbitrary fp32 numbers, so the tensor cores can add up one block of 128 only; S_b goes from tensor
 // memory to registers, where the running sum is kept in fp32: one fma per output and block, 1/128 of the MMA's
-// multiply-adds on pipes of 1/64 of its rate.  sa sb is rounded to fp32 before it meets S_b, by a warp that has the time for it (the sums have none
-// for a second multiplication): below 2^-126 that costs bits, and a product that is infinite is reported (PSB_ERR_RANGE).
+// multiply-adds on pipes of 1/64 of its rate.  sa sb is rounded to fp32 before it meets S_b, by a warp of its own (a second multiplication in the
+// sums would double their arithmetic): below 2^-126 that costs bits, and a product that is infinite is reported (PSB_ERR_RANGE).
 //
 // Many rows (gemm_fp8_kernel): one persistent CTA an SM, or a pair of SMs on one tile (cta_group::2).  Warps of their own copy a, copy
 // b, issue the MMAs and multiply the scales; eight warps add up a block of 128 or 256 columns out of one TMEM buffer while the
-// MMAs of the next block fill the other, and hand finished tiles to the copy engine.  8192^3: 500 us (2.2 PFLOP/s; the clocks sink
-// to 1.65 GHz under the power cap in a long stream of calls).  A block of 256 x 256 x 128 takes about 950 clocks, 512 of them the
-// MMAs'; in an earlier state, with one of four MMAs and neither fmas nor output, it took 650: the wait for the MMAs, the loads from TMEM
-// and the hand-over follow one another, and two buffers are all that TMEM holds.  Measured and dropped: sixteen summing warps
+// MMAs of the next block fill the other, and hand finished tiles to the copy engine.  8192^3: 597 us in a long stream of
+// calls (1.84 PFLOP/s; the clocks sink to 1.65 GHz under the power cap), 500 in the first calls on a cool chip (as the times below
+// were taken).  A block of 256 x 256 x 128 takes about 950 clocks, 512 of them the MMAs'; in an earlier state, with one of four MMAs and neither
+// fmas nor output, it took 650: the wait for the MMAs, the loads from TMEM and the hand-over follow one another, and two buffers are all
+// that TMEM holds.  Measured and dropped: sixteen summing warps
 // (as fast), halves of the columns handed over one by one (604 us against 576), two warps that issue MMAs (no change), 128 x 256 on
 // single SMs (600), a block's first columns fetched before the last arithmetic of the block before it (575 against 560), polls
 // that read a clock, more code anywhere in the summing warps (154 KB of it cost 5400 clocks a tile).
@@ -1029,9 +1030,9 @@ psb_status launch_gemm_fp8(psb_ctx* ctx, const Fp8GemmArgs& given, void* scratch
     return launch_stream<64>(ctx, a, s);
   // Tiles of 256 x 256 by pairs of SMs read half of the bytes per product that single SMs' 128 x 128 do, and take 1.65 times as long a
   // block for twice an SM's work; what counts is the number of rounds of tiles (in halves: a run of an expert ends in the middle of a
-  // tile).  us, pairs against singles: 8192^3 523 and 622, 4096^3 90 and 96, 1500 x 1000 x 2048 18.6 and 12.3, 3000 x 2500 x 1000
-  // 27.4 and 32.3, 512 x 4096 x 4096 24.6 and 17.6; 16384 rows over 8 experts of 4096 x 4096 300 and 340, over 64 of 2048 x 2048 163 and 147,
-  // 1884 over 18 of 2048 x 3344 68 and 50.
+  // tile).  us in a stream of calls of a second, pairs against singles: 8192^3 597 and 741, 4096^3 86 and 96, 1500 x 1000 x 2048 16.2 and 10.6,
+  // 3000 x 2500 x 1000 24.0 and 25.8, 512 x 4096 x 4096 21.7 and 14.6; 16384 rows over 8 experts of 4096 x 4096 386 and 433, over 64 of
+  // 2048 x 2048 190 and 177, 1884 over 18 of 2048 x 3344 70 and 57.
   const uint64_t sms = (uint64_t)ctx->sm_count, of = a.experts ? a.experts : 1u;
   auto rounds = [&](uint32_t tile, uint64_t at_once) {
     const uint64_t part = 2u * (uint64_t)each / tile + 1u, halves = !a.experts ? 2u * ((each + tile - 1u) / tile) : part < 2u ? 2u : part;
