@@ -426,6 +426,7 @@ psb_status psb_sample_level_static(const float* w_dev, const psb_wshape* shape,
  *   top   = 448 (PSB_DT_E4M3) or 57344 (PSB_DT_E5M2)
  *   scale = max(max |x| / top, 2^-126)      over the block's finite values, fp32
  *   code  = round(x * (1 / scale))          ties to even, saturating at +-top; Inf and NaN become NaN
+ * Quotient, reciprocal and product are fp32 operations, each rounded once.
  * codes_dev: one byte each; scales_dev: [ceil(rows / block_rows)][ceil(cols / 128)].
  * Rows of codes that psb_gemm_fp8 is to read start at multiples of 16 bytes. */
 typedef struct {
